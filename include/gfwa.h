@@ -1,6 +1,6 @@
 /*
  * gfwa.h -- C ABI of libgfwa: GatedFWA (memory-gated sliding-window softmax attention)
- * for AMD MI355X (gfx950).
+ * for AMD MI355X (gfx950).  The operators that a model's layer has directly around it stand in gfwa_layer.h.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -49,7 +49,8 @@ typedef enum {
     GFWA_ERR_WORKSPACE = -5,   /* workspace NULL or smaller than the matching gfwa_*_workspace_bytes() call
                                   (backward, decode, scan-then-propagate) asks for; gfwa_decode_static:
                                   the sizes need more than the library's own scratch holds */
-    GFWA_ERR_HIP = -6          /* the HIP runtime refused a launch; see gfwa_strerror */
+    GFWA_ERR_HIP = -6,         /* the HIP runtime refused a launch; see gfwa_strerror */
+    GFWA_ERR_OVERLAP = -7      /* an output overlaps an input, or its own rows (gfwa_layer.h) */
 } gfwa_status_t;
 
 /*
@@ -220,14 +221,16 @@ int gfwa_version(void);
  * Instrumentation (not part of the method): per-kernel timing with HIP events recorded on the
  * caller's stream around every kernel the library launches.  gfwa_profile_enable(1) clears the
  * records and starts recording (at most 8192 launches are kept), gfwa_profile_enable(0) stops.
- * gfwa_profile_read waits for the recorded events and returns, per kernel id k in [0, 13), the
- * summed duration in milliseconds and the number of launches; n must be >= 13.  Kernel ids:
+ * gfwa_profile_read waits for the recorded events and returns, per kernel id k in [0, n), the
+ * summed duration in milliseconds and the number of launches; n must be >= 13, there are 19.  Kernel ids:
  * 0 gate prefix scan, 1 forward, 2 backward row-dot (D), 3 backward dK/dV, 4 backward dQ,
  * 5 gate-gradient reverse scan, 6 gate activation + prefix scan, 7 gate activation backward,
  * 8 decoding step (per-chunk partials), 9 decoding step (merge of the chunks), 10 and 11 the two
  * launches of gfwa_gate_prefix_stp (segment sums, scan of the segments; one launch is id 0, with the activation
  * id 6), 12 the segment sums of the
- * gate-gradient scan when the backward cuts few long rows into segments (its scan is then id 5).
+ * gate-gradient scan when the backward cuts few long rows into segments (its scan is then id 5); of gfwa_layer.h 13 norm and
+ * rotation, 14 its derivative, 15 the sums of the norm weights' gradients, 16 append to the paged cache, 17 and 18 decoding
+ * step on the paged cache (per-chunk partials, merge of the chunks).
  * A launch that takes the norms of the keys in front of the forward is part of id 1; in front of the split
  * kernels of small bf16 backwards the one that takes them is part of the pass behind it, id 4 or 3.
  * Where both passes of the backward go in one launch (fp32, and small bf16 problems) id 3 is that launch and

@@ -1,4 +1,4 @@
-"""Python binding with the same names as the C ABI (include/gfwa.h).
+"""Python binding with the same names as the C ABI (include/gfwa.h, include/gfwa_layer.h).
 
 Each function takes torch tensors living on the GPU, checks shapes/dtypes/contiguity on the
 host, and passes raw device pointers and the current HIP stream to the library.  There is no
@@ -26,15 +26,23 @@ _call = None  # the native module, bound to _lib's functions
 # the functions it calls, in the order its bind() expects them
 _CALLED = ("gfwa_gate_prefix", "gfwa_gate_activation_prefix", "gfwa_gate_activation_backward",
            "gfwa_gate_scan_workspace_bytes", "gfwa_gate_prefix_stp", "gfwa_forward_gqa", "gfwa_backward_workspace_bytes",
-           "gfwa_backward_gqa", "gfwa_decode_workspace_bytes", "gfwa_decode", "gfwa_decode_static")
+           "gfwa_backward_gqa", "gfwa_decode_workspace_bytes", "gfwa_decode", "gfwa_decode_static", "gfwa_qk_norm_rope",
+           "gfwa_qk_norm_rope_backward_workspace_bytes", "gfwa_qk_norm_rope_backward", "gfwa_append_paged", "gfwa_decode_paged_workspace_bytes",
+           "gfwa_decode_paged")
 
 GFWA_BF16, GFWA_F32 = 0, 1
 
 EXPORTS = ("gfwa_gate_prefix", "gfwa_gate_activation_prefix", "gfwa_gate_activation_backward", "gfwa_forward", "gfwa_backward_workspace_bytes", "gfwa_backward_fast_workspace_bytes", "gfwa_backward",
            "gfwa_forward_gqa", "gfwa_backward_gqa", "gfwa_decode_workspace_bytes", "gfwa_decode", "gfwa_decode_static", "gfwa_gate_scan_workspace_bytes", "gfwa_gate_prefix_stp",
            "gfwa_strerror", "gfwa_version", "gfwa_probe_mfma", "gfwa_probe_copy", "gfwa_profile_enable", "gfwa_profile_read",
-           "gfwa_profile_kernel_name")
-N_KERNELS = 13
+           "gfwa_profile_kernel_name", "gfwa_qk_norm_rope", "gfwa_qk_norm_rope_backward_workspace_bytes", "gfwa_qk_norm_rope_backward",
+           "gfwa_append_paged", "gfwa_decode_paged_workspace_bytes", "gfwa_decode_paged")
+N_KERNELS = 19
+
+
+class GfwaHeads(ctypes.Structure):
+    """gfwa_heads_t: a strided tensor of heads, strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_longlong), ("token", ctypes.c_longlong), ("head", ctypes.c_longlong)]
 
 
 class GfwaError(RuntimeError):
@@ -87,6 +95,19 @@ def load_library() -> ctypes.CDLL:
     lib.gfwa_gate_scan_workspace_bytes.restype = ctypes.c_size_t
     lib.gfwa_gate_prefix_stp.argtypes = [fp, fp, f, fp, vp, ctypes.c_size_t, i, i, i, vp]
     lib.gfwa_gate_prefix_stp.restype = i
+    hp, ll, z = ctypes.POINTER(GfwaHeads), ctypes.c_longlong, ctypes.c_size_t
+    lib.gfwa_qk_norm_rope.argtypes = [i, hp, hp, hp, fp, fp, f, vp, i, vp, i, vp, vp, vp, i, i, i, i, i, vp]
+    lib.gfwa_qk_norm_rope.restype = i
+    lib.gfwa_qk_norm_rope_backward_workspace_bytes.argtypes = [i, i, i, i, i]
+    lib.gfwa_qk_norm_rope_backward_workspace_bytes.restype = z
+    lib.gfwa_qk_norm_rope_backward.argtypes = [i, hp, hp, fp, fp, f, vp, i, vp, i, vp, vp, vp, hp, hp, hp, fp, fp, vp, z, i, i, i, i, i, vp]
+    lib.gfwa_qk_norm_rope_backward.restype = i
+    lib.gfwa_append_paged.argtypes = [i, hp, hp, hp, fp, fp, f, vp, i, i, fp, ll, ll, vp, vp, vp, vp, vp, vp, fp, i, i, i, i, i, i, i, i, vp]
+    lib.gfwa_append_paged.restype = i
+    lib.gfwa_decode_paged_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+    lib.gfwa_decode_paged_workspace_bytes.restype = z
+    lib.gfwa_decode_paged.argtypes = [i, vp, vp, vp, fp, vp, vp, vp, fp, vp, z, i, i, i, i, i, i, i, i, f, vp]
+    lib.gfwa_decode_paged.restype = i
     lib.gfwa_probe_mfma.argtypes = [fp, i, i, i, ctypes.POINTER(ctypes.c_double), vp]
     lib.gfwa_probe_mfma.restype = i
     lib.gfwa_probe_copy.argtypes = [vp, vp, ctypes.c_size_t, vp]
@@ -234,6 +255,57 @@ def gfwa_decode_static(q: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, c: t
     """gfwa_decode without a workspace and without any allocation: the caller passes the outputs
     o [B,H,d] and L [B,H]; the partial results live in the library's own scratch."""
     return (_call or _native()).decode_static(q, Kc, Vc, c, pos, w, scale, alpha_t, o, L)
+
+
+def gfwa_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
+                      wk: Optional[torch.Tensor] = None, eps: float = 1e-6, freq: Optional[torch.Tensor] = None,
+                      pos: Optional[torch.Tensor] = None, norm: bool = True, paired: bool = False, Q: Optional[torch.Tensor] = None,
+                      K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
+    """Norm and rotation of query and key heads, in the layout the attention reads.  q [B,N,H,d], k, v [B,N,Hkv,d]: any strides with a
+    contiguous last dimension and rows on 16 bytes (views of one packed projection); weights [d] fp32; freq [rot/2] fp64: radians for each
+    position (None: no rotation); pos [B,N] int32 (None: 0 .. N-1); norm=False: no norm; paired: dimensions (2j, 2j+1) turn together instead
+    of (j, j + rot/2).  Returns Q [B,H,N,d], K, V [B,Hkv,N,d] (V None without v)."""
+    return (_call or _native()).qk_norm_rope(q, k, v, wq, wk, eps, freq, norm, paired, pos, Q, K, V)
+
+
+def gfwa_qk_norm_rope_backward_workspace_bytes(B: int, H: int, Hkv: int, N: int, d: int) -> int:
+    return int(load_library().gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d))
+
+
+def gfwa_qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, dQ: torch.Tensor, dK: torch.Tensor, dV: Optional[torch.Tensor] = None,
+                               wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                               freq: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, norm: bool = True,
+                               paired: bool = False, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                               dv: Optional[torch.Tensor] = None, dwq: Optional[torch.Tensor] = None,
+                               dwk: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Derivative of gfwa_qk_norm_rope, whose arguments q .. paired are.  dQ [B,H,N,d], dK, dV [B,Hkv,N,d] dense; dq, dk, dv: strided outputs of
+    q's and k's shapes (views of one packed gradient) or None.  Returns dq, dk, dv (None without dV), dwq, dwk ([d] fp32, each None without
+    its weight unless an output for it is given)."""
+    return (_call or _native()).qk_norm_rope_backward(q, k, dQ, dK, dV, wq, wk, eps, freq, norm, paired, pos, dq, dk, dv, dwq, dwk, workspace)
+
+
+def gfwa_append_paged(k: torch.Tensor, v: torch.Tensor, Kp: torch.Tensor, Vp: torch.Tensor, start: torch.Tensor, cached: torch.Tensor,
+                      table: torch.Tensor, q: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
+                      wk: Optional[torch.Tensor] = None, eps: float = 1e-6, freq: Optional[torch.Tensor] = None, norm: bool = True,
+                      paired: bool = False, alpha: Optional[torch.Tensor] = None, cp: Optional[torch.Tensor] = None,
+                      Q: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Append new tokens to a paged cache: rows start[b] .. start[b+1] of k, v [rows,Hkv,d] (and q [rows,H,d], strided as in
+    gfwa_qk_norm_rope) go to positions cached[b] on of sequence b, normed and rotated; with alpha [rows,H] (any strides) the gate prefix is
+    carried on in cp.  Kp, Vp [pages,Hkv,page,d], cp [pages,H,page] fp32, table [B,max_pages] int32; start [B+1], cached [B] int32.
+    Returns Q [rows,H,d] (None without q); rows of no sequence are left as they are (a fresh Q: undefined)."""
+    return (_call or _native()).append_paged(k, v, Kp, Vp, start, cached, table, q, wq, wk, eps, freq, norm, paired, alpha, cp, Q)
+
+
+def gfwa_decode_paged_workspace_bytes(B: int, H: int, Hkv: int, d: int, page: int, max_pages: int, w: int) -> int:
+    return int(load_library().gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, int(w)))
+
+
+def gfwa_decode_paged(q: torch.Tensor, Kp: torch.Tensor, Vp: torch.Tensor, cp: torch.Tensor, table: torch.Tensor, pos: torch.Tensor,
+                      w: int, scale: float, o: Optional[torch.Tensor] = None, L: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """One decoding step against a paged cache (gfwa_append_paged's): q [B,H,d] at positions pos [B] int32, whose keys are appended
+    already; -1: a slot without a sequence (o = 0, L = -inf).  Returns o [B,H,d], L [B,H]."""
+    return (_call or _native()).decode_paged(q, Kp, Vp, cp, table, pos, w, scale, o, L, workspace)
 
 
 def gfwa_probe_mfma(sink: torch.Tensor, iterations: int, workgroups: int, random_operands: int = 0) -> float:

@@ -5,8 +5,10 @@
 #include <string.h>
 #include <atomic>
 #include <mutex>
+#include <utility>
 
 #include "../../include/gfwa.h"
+#include "../../include/gfwa_layer.h"
 #include "gfwa_internal.h"
 
 namespace gfwa {
@@ -31,6 +33,77 @@ static int check_dims(int B, int H, int N, int d, int w, bool need_d) {
     if (need_d && d != 64 && d != 128) return GFWA_ERR_UNSUPPORTED;
     return GFWA_OK;
 }
+
+// ---- what the operators around the attention check
+static constexpr long long kMostOffset = 1LL << 40;  // elements: far beyond the memory there is, and safe to multiply
+
+static int check_layer_dims(int B, int H, int Hkv, int N, int d) {
+    if (int r = check_dims(B, H, N, d, 1, true)) return r;
+    if (Hkv <= 0 || H % Hkv != 0 || (long long)B * N > 0x7fffffffLL) return GFWA_ERR_DIM;
+    return GFWA_OK;
+}
+
+static int check_rotation(int dt, float eps, int rot, int flags, int d) {
+    if (dt != GFWA_BF16 && dt != GFWA_F32) return GFWA_ERR_UNSUPPORTED;
+    if (flags & ~(GFWA_HEAD_NORM | GFWA_ROPE_PAIRED)) return GFWA_ERR_UNSUPPORTED;
+    if (rot < 0 || rot > d || rot % 16 != 0 || ((flags & GFWA_HEAD_NORM) && !(eps >= 0.0f))) return GFWA_ERR_DIM;
+    return GFWA_OK;
+}
+
+// positions are 32-bit, offsets into the cache 64-bit
+static int check_cache(int B, int H, int pages, int page, int max_pages) {
+    if (B <= 0 || pages <= 0 || page <= 0 || page % 16 != 0 || max_pages <= 0) return GFWA_ERR_DIM;
+    if ((long long)B * H > (1LL << 24) || (long long)max_pages * page > 0x7fffffffLL) return GFWA_ERR_DIM;
+    return GFWA_OK;
+}
+
+struct Bytes {
+    const void* at;
+    size_t count;
+    bool meets(const Bytes& o) const { return at && o.at && overlap(at, count, o.at, o.count); }
+};
+
+// The strided tensor of `heads` heads that a caller describes; nullptr: none.
+struct HeadsSpan {
+    const gfwa_heads_t* t;
+    int heads;
+    int check(int B, int N, int d, size_t size) const {
+        if (!t) return GFWA_OK;
+        if (!aligned(t->data, 16)) return GFWA_ERR_ALIGN;
+        const long long unit = 16 / (long long)size, strides[] = {t->batch, t->token, t->head}, counts[] = {B, N, heads};
+        double last = 0;
+        for (int i = 0; i < 3; ++i) {
+            if (counts[i] == 1) continue;
+            if (strides[i] < 0 || strides[i] > kMostOffset) return GFWA_ERR_DIM;
+            if (strides[i] % unit != 0) return GFWA_ERR_ALIGN;
+            last += (double)strides[i] * (double)(counts[i] - 1);
+        }
+        return last > (double)kMostOffset ? GFWA_ERR_DIM : GFWA_OK;
+    }
+    long long last_row(int B, int N) const {
+        return (B > 1 ? t->batch * (B - 1) : 0) + (N > 1 ? t->token * (N - 1) : 0) + (heads > 1 ? t->head * (heads - 1) : 0);
+    }
+    Bytes bytes(int B, int N, int d, size_t size) const {
+        return t ? Bytes{t->data, (size_t)(last_row(B, N) + d) * size} : Bytes{nullptr, 0};
+    }
+    // whether no two rows share an element: taken by stride, each dimension steps over all of the one below it
+    bool rows_disjoint(int B, int N, int d) const {
+        if (!t) return true;
+        long long dims[3][2] = {{t->batch, B}, {t->token, N}, {t->head, heads}};
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2 - i; ++j)
+                if (dims[j][0] > dims[j + 1][0]) std::swap(dims[j], dims[j + 1]);
+        long long reach = d;
+        for (auto& x : dims) {
+            if (x[1] == 1) continue;
+            if (x[0] < reach) return false;
+            reach += x[0] * (x[1] - 1);
+        }
+        return true;
+    }
+};
+
+static HeadsView view(const gfwa_heads_t* t) { return t ? HeadsView{t->data, t->batch, t->token, t->head} : HeadsView{nullptr, 0, 0, 0}; }
 
 // ---- optional per-kernel timing with HIP events on the caller's stream ----
 namespace {
@@ -241,6 +314,142 @@ int gfwa_decode_static(gfwa_dtype_t dt, const void* q, const void* Kc, const voi
                              stream));
 }
 
+// ---- around the attention (gfwa_layer.h)
+
+size_t gfwa_qk_norm_rope_backward_workspace_bytes(int B, int H, int Hkv, int N, int d) {
+    if (check_layer_dims(B, H, Hkv, N, d) != GFWA_OK) return 0;
+    return qk_norm_rope_backward_workspace_bytes(d);
+}
+
+int gfwa_qk_norm_rope(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfwa_heads_t* k, const gfwa_heads_t* v, const float* wq,
+                      const float* wk, float eps, const double* freq, int rot, const int* pos, int flags, void* Q, void* K,
+                      void* V, int B, int H, int Hkv, int N, int d, gfwa_stream_t stream) {
+    if (!q || !q->data || !k || !k->data || (v && (!v->data || !V)) || !Q || !K || (rot > 0 && !freq)) return GFWA_ERR_NULL;
+    if (int r = check_layer_dims(B, H, Hkv, N, d)) return r;
+    if (int r = check_rotation(dt, eps, rot, flags, d)) return r;
+    const size_t size = dt == GFWA_BF16 ? 2 : 4, bytes = (size_t)B * N * d * size;
+    const HeadsSpan spans[] = {{q, H}, {k, Hkv}, {v, Hkv}};
+    for (const HeadsSpan& x : spans)
+        if (int r = x.check(B, N, d, size)) return r;
+    if (!v) V = nullptr;
+    const Bytes outs[] = {{Q, bytes * H}, {K, bytes * Hkv}, {V, bytes * Hkv}};
+    for (const Bytes& o : outs)
+        if (!aligned(o.at, 16)) return GFWA_ERR_ALIGN;
+    if (!aligned(wq, 4) || !aligned(wk, 4) || !aligned(pos, 4) || (rot > 0 && !aligned(freq, 8))) return GFWA_ERR_ALIGN;
+    for (int i = 0; i < 3; ++i) {
+        for (const HeadsSpan& x : spans)
+            if (outs[i].meets(x.bytes(B, N, d, size))) return GFWA_ERR_OVERLAP;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].meets(outs[j])) return GFWA_ERR_OVERLAP;
+    }
+    const HeadRotation how{wq, wk, eps, freq, rot, pos, (flags & GFWA_HEAD_NORM) != 0, (flags & GFWA_ROPE_PAIRED) != 0};
+    return hip_status(qk_norm_rope(dt == GFWA_BF16, view(q), view(k), view(v), how, Q, K, V, B, H, Hkv, N, d, stream));
+}
+
+int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfwa_heads_t* k, const float* wq, const float* wk,
+                               float eps, const double* freq, int rot, const int* pos, int flags, const void* dQ, const void* dK,
+                               const void* dV, const gfwa_heads_t* dq, const gfwa_heads_t* dk, const gfwa_heads_t* dv, float* dwq,
+                               float* dwk, void* workspace, size_t workspace_bytes, int B, int H, int Hkv, int N, int d,
+                               gfwa_stream_t stream) {
+    const bool norm = (flags & GFWA_HEAD_NORM) != 0;
+    if (!dQ || !dK || !dq || !dq->data || !dk || !dk->data || (norm && (!q || !q->data || !k || !k->data)) || (rot > 0 && !freq)) return GFWA_ERR_NULL;
+    if ((dV != nullptr) != (dv != nullptr && dv->data != nullptr)) return GFWA_ERR_NULL;
+    if (int r = check_layer_dims(B, H, Hkv, N, d)) return r;
+    if (int r = check_rotation(dt, eps, rot, flags, d)) return r;
+    if (!norm && (dwq || dwk)) return GFWA_ERR_UNSUPPORTED;
+    if (!norm) q = k = nullptr;
+    if (!dV) dv = nullptr;
+    const size_t size = dt == GFWA_BF16 ? 2 : 4, bytes = (size_t)B * N * d * size;
+    const HeadsSpan ins[] = {{q, H}, {k, Hkv}}, outs[] = {{dq, H}, {dk, Hkv}, {dv, Hkv}};
+    for (const HeadsSpan& x : ins)
+        if (int r = x.check(B, N, d, size)) return r;
+    for (const HeadsSpan& x : outs) {
+        if (int r = x.check(B, N, d, size)) return r;
+        if (!x.rows_disjoint(B, N, d)) return GFWA_ERR_OVERLAP;
+    }
+    const Bytes grads[] = {{dQ, bytes * H}, {dK, bytes * Hkv}, {dV, bytes * Hkv}};
+    for (const Bytes& g : grads)
+        if (!aligned(g.at, 16)) return GFWA_ERR_ALIGN;
+    if (!aligned(wq, 4) || !aligned(wk, 4) || !aligned(pos, 4) || !aligned(dwq, 4) || !aligned(dwk, 4) || (rot > 0 && !aligned(freq, 8)))
+        return GFWA_ERR_ALIGN;
+    for (const HeadsSpan& o : outs) {
+        for (const HeadsSpan& x : ins)
+            if (o.bytes(B, N, d, size).meets(x.bytes(B, N, d, size))) return GFWA_ERR_OVERLAP;
+        for (const Bytes& g : grads)
+            if (o.bytes(B, N, d, size).meets(g)) return GFWA_ERR_OVERLAP;
+    }
+    if (dwq || dwk) {
+        if (!workspace || workspace_bytes < gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d)) return GFWA_ERR_WORKSPACE;
+        if (!aligned(workspace, 16)) return GFWA_ERR_ALIGN;
+    }
+    const HeadRotation how{wq, wk, eps, freq, rot, pos, norm, (flags & GFWA_ROPE_PAIRED) != 0};
+    return hip_status(qk_norm_rope_backward(dt == GFWA_BF16, view(q), view(k), how, dQ, dK, dV, view(dq), view(dk), view(dv), dwq, dwk,
+                                            (float*)workspace, B, H, Hkv, N, d, stream));
+}
+
+int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfwa_heads_t* k, const gfwa_heads_t* v, const float* wq,
+                      const float* wk, float eps, const double* freq, int rot, int flags, const float* alpha, long long alpha_token,
+                      long long alpha_head, const int* start, const int* cached, const int* table, void* Q, void* Kp, void* Vp,
+                      float* cp, int rows, int B, int H, int Hkv, int d, int pages, int page, int max_pages,
+                      gfwa_stream_t stream) {
+    if ((q && (!q->data || !Q)) || !k || !k->data || !v || !v->data || (alpha && !cp) || !start || !cached || !table || !Kp || !Vp ||
+        (rot > 0 && !freq))
+        return GFWA_ERR_NULL;
+    if (int r = check_layer_dims(1, H, Hkv, rows, d)) return r;
+    if (int r = check_cache(B, H, pages, page, max_pages)) return r;
+    if (int r = check_rotation(dt, eps, rot, flags, d)) return r;
+    const size_t size = dt == GFWA_BF16 ? 2 : 4;
+    if (!q) Q = nullptr;
+    if (!alpha) cp = nullptr;
+    const HeadsSpan ins[] = {{q, H}, {k, Hkv}, {v, Hkv}};
+    for (const HeadsSpan& x : ins)
+        if (int r = x.check(1, rows, d, size)) return r;
+    if (alpha) {
+        if (alpha_token < 0 || alpha_head < 0 || alpha_token > kMostOffset || alpha_head > kMostOffset ||
+            (double)(rows - 1) * alpha_token + (double)(H - 1) * alpha_head > (double)kMostOffset)
+            return GFWA_ERR_DIM;
+    }
+    if (!aligned(Q, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) || !aligned(cp, 4) || !aligned(alpha, 4) || !aligned(start, 4) ||
+        !aligned(cached, 4) || !aligned(table, 4) || !aligned(wq, 4) || !aligned(wk, 4) || (rot > 0 && !aligned(freq, 8)))
+        return GFWA_ERR_ALIGN;
+    const size_t per_head = (size_t)pages * page;
+    const Bytes outs[] = {{Q, (size_t)rows * H * d * size}, {Kp, per_head * Hkv * d * size}, {Vp, per_head * Hkv * d * size}, {cp, per_head * H * 4}};
+    const Bytes gate{alpha, alpha ? 4 * (size_t)((rows - 1) * alpha_token + (H - 1) * alpha_head + 1) : 0};
+    for (int i = 0; i < 4; ++i) {
+        for (const HeadsSpan& x : ins)
+            if (outs[i].meets(x.bytes(1, rows, d, size))) return GFWA_ERR_OVERLAP;
+        if (outs[i].meets(gate)) return GFWA_ERR_OVERLAP;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].meets(outs[j])) return GFWA_ERR_OVERLAP;
+    }
+    const HeadRotation how{wq, wk, eps, freq, rot, nullptr, (flags & GFWA_HEAD_NORM) != 0, (flags & GFWA_ROPE_PAIRED) != 0};
+    const PagedCache cache{Kp, Vp, cp, table, pages, page, max_pages};
+    return hip_status(append_paged(dt == GFWA_BF16, view(q), view(k), view(v), how, alpha, alpha_token, alpha_head, start, cached, Q, cache, rows,
+                                   B, H, Hkv, d, stream));
+}
+
+size_t gfwa_decode_paged_workspace_bytes(int B, int H, int Hkv, int d, int page, int max_pages, int w) {
+    if (check_layer_dims(B, H, Hkv, 1, d) != GFWA_OK || check_cache(B, H, 1, page, max_pages) != GFWA_OK || w < 1) return 0;
+    return (decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, w) + 255) & ~(size_t)255;
+}
+
+int gfwa_decode_paged(gfwa_dtype_t dt, const void* q, const void* Kp, const void* Vp, const float* cp, const int* table,
+                      const int* pos, void* o, float* L, void* workspace, size_t workspace_bytes, int B, int H, int Hkv, int d,
+                      int pages, int page, int max_pages, int w, float scale, gfwa_stream_t stream) {
+    if (!q || !Kp || !Vp || !cp || !table || !pos || !o) return GFWA_ERR_NULL;
+    if (int r = check_layer_dims(B, H, Hkv, 1, d)) return r;
+    if (int r = check_cache(B, H, pages, page, max_pages)) return r;
+    if (w < 1) return GFWA_ERR_DIM;
+    if (dt != GFWA_BF16 && dt != GFWA_F32) return GFWA_ERR_UNSUPPORTED;
+    if (!aligned(q, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) || !aligned(o, 16) || !aligned(cp, 4) || !aligned(table, 4) ||
+        !aligned(pos, 4) || !aligned(L, 4))
+        return GFWA_ERR_ALIGN;
+    if (!workspace || workspace_bytes < gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, w)) return GFWA_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return GFWA_ERR_ALIGN;
+    const PagedCache cache{const_cast<void*>(Kp), const_cast<void*>(Vp), const_cast<float*>(cp), table, pages, page, max_pages};
+    return hip_status(decode_paged(dt == GFWA_BF16, q, cache, pos, o, L, (float*)workspace, B, H, Hkv, d, w, scale, stream));
+}
+
 const char* gfwa_strerror(int code) {
     switch (code) {
         case GFWA_OK: return "ok";
@@ -252,6 +461,7 @@ const char* gfwa_strerror(int code) {
             return "workspace missing or smaller than the matching gfwa_*_workspace_bytes() call asks for; for "
                    "gfwa_decode_static: the sizes need more than the library's 32 MiB of scratch";
         case GFWA_ERR_HIP: return g_hip_msg;
+        case GFWA_ERR_OVERLAP: return "an output overlaps an input, or its own rows overlap";
         default: return "unknown status code";
     }
 }
@@ -283,13 +493,14 @@ int gfwa_profile_enable(int on) {
 
 int gfwa_profile_read(float* total_ms, int* launches, int n) {
     if (!total_ms || !launches) return GFWA_ERR_NULL;
-    if (n < kKernCount) return GFWA_ERR_DIM;
+    if (n < kKernFirstCount) return GFWA_ERR_DIM;
     for (int k = 0; k < n; ++k) {
         total_ms[k] = 0.f;
         launches[k] = 0;
     }
     std::lock_guard<std::mutex> hold(g_prof.lock);
     for (int i = 0; i < g_prof.used; ++i) {
+        if (g_prof.rec[i].kernel >= n) continue;
         hipError_t e = hipEventSynchronize(g_prof.rec[i].stop);
         float ms = 0.f;
         if (e == hipSuccess) e = hipEventElapsedTime(&ms, g_prof.rec[i].start, g_prof.rec[i].stop);
@@ -304,7 +515,8 @@ const char* gfwa_profile_kernel_name(int k) {
     static const char* names[kKernCount] = {"gate_prefix_scan", "forward", "bwd_rowdot", "bwd_dkv", "bwd_dq",
                                             "gate_grad_scan", "gate_activation_prefix_scan",
                                             "gate_activation_bwd", "decode_partial", "decode_combine", "scan_segment_sum", "scan_propagate",
-                                            "gate_grad_segment_sum"};
+                                            "gate_grad_segment_sum", "qk_norm_rope", "qk_norm_rope_bwd", "norm_weight_grad_sum", "append_paged",
+                                            "decode_paged_partial", "decode_paged_combine"};
     return (k >= 0 && k < kKernCount) ? names[k] : "";
 }
 

@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
@@ -16,9 +17,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
+#include <optional>
 #include <string>
 
 #include "../../include/gfwa.h"
+#include "../../include/gfwa_layer.h"
 
 namespace {
 
@@ -35,6 +38,12 @@ struct Library {
     decltype(&gfwa_decode_workspace_bytes) decode_workspace_bytes;
     decltype(&gfwa_decode) decode;
     decltype(&gfwa_decode_static) decode_static;
+    decltype(&gfwa_qk_norm_rope) qk_norm_rope;
+    decltype(&gfwa_qk_norm_rope_backward_workspace_bytes) qk_norm_rope_backward_workspace_bytes;
+    decltype(&gfwa_qk_norm_rope_backward) qk_norm_rope_backward;
+    decltype(&gfwa_append_paged) append_paged;
+    decltype(&gfwa_decode_paged_workspace_bytes) decode_paged_workspace_bytes;
+    decltype(&gfwa_decode_paged) decode_paged;
 };
 constexpr Py_ssize_t kFunctions = sizeof(Library) / sizeof(void*);
 Library lib;
@@ -404,6 +413,311 @@ PyObject* decode_static(PyObject* const* a) {  // q, Kc, Vc, c, pos, w, scale, a
     return PyTuple_Pack(2, a[8], a[9]);
 }
 
+// ---- around the attention (gfwa_layer.h)
+
+// Every tensor of a call on one GPU, and that the current one: its current stream is where the call goes.
+struct OneDevice {
+    at::Device device;
+    explicit OneDevice(const at::Tensor& t) : device(t.device()) {}
+    void also(const at::Tensor& t, const char* name) const {
+        if (t.device() != device)
+            fail(PyExc_ValueError, std::string(name) + " is on " + t.device().str() + ", the first tensor on " + device.str());
+    }
+    void is_current() const {
+        const int now = c10::hip::current_device();
+        if (device.index() != now)
+            fail(PyExc_ValueError, "the tensors are on " + device.str() + ", the current device is " + std::to_string(now));
+    }
+};
+
+const at::Tensor& dense(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const OneDevice& dev, const char* name) {
+    const at::Tensor& t = tensor_of(o, name);
+    need(t, shape, dtype, name);
+    dev.also(t, name);
+    return t;
+}
+const void* optional_input(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const OneDevice& dev, const char* name) {
+    return o == Py_None ? nullptr : dense(o, shape, dtype, dev, name).const_data_ptr();
+}
+int sizes_to_int(int64_t n, const char* what) {
+    if (n > 0x7fffffffLL) fail(PyExc_ValueError, std::string(what) + " is too large");
+    return (int)n;
+}
+
+// A strided tensor of heads, [B,N,heads,d] (or [rows,heads,d]): anything whose last dimension is contiguous.
+struct Heads {
+    gfwa_heads_t t{};
+    bool given = false;
+    Heads() = default;
+    Heads(const at::Tensor& x, at::IntArrayRef shape, at::ScalarType dtype, const OneDevice& dev, const char* name, bool write) {
+        if (!x.is_cuda()) fail(PyExc_ValueError, std::string(name) + " must live on the GPU");
+        if (x.sizes() != shape)
+            fail(PyExc_ValueError, std::string(name) + " has shape " + shape_text(x.sizes()) + ", expected " + shape_text(shape));
+        if (x.scalar_type() != dtype)
+            fail(PyExc_TypeError, std::string(name) + " has dtype " + dtype_text(x.scalar_type()) + ", expected " + dtype_text(dtype));
+        const int64_t n = x.dim();
+        if (x.stride(n - 1) != 1) fail(PyExc_ValueError, std::string(name) + " must be contiguous in its last dimension");
+        dev.also(x, name);
+        t.data = write ? x.data_ptr() : const_cast<void*>(x.const_data_ptr());
+        t.head = x.stride(n - 2);
+        t.token = x.stride(n - 3);
+        t.batch = n == 4 ? x.stride(0) : 0;
+        given = true;
+    }
+    const gfwa_heads_t* get() const { return given ? &t : nullptr; }
+};
+
+// Norm and rotation: wq, wk, eps, freq, norm, paired
+struct Rotation {
+    const float *wq, *wk;
+    float eps;
+    const double* freq = nullptr;
+    int rot = 0, flags = 0;
+    Rotation(PyObject* const* a, int64_t d, const OneDevice& dev) {
+        const int64_t weights[1] = {d};
+        wq = (const float*)optional_input(a[0], weights, at::kFloat, dev, "wq");
+        wk = (const float*)optional_input(a[1], weights, at::kFloat, dev, "wk");
+        eps = as_float(a[2]);
+        if (a[3] != Py_None) {
+            const at::Tensor& f = tensor_of(a[3], "freq");
+            if (f.dim() != 1) fail(PyExc_ValueError, "freq must be [rot / 2]");
+            const int64_t half[1] = {f.size(0)};
+            freq = (const double*)dense(a[3], half, at::kDouble, dev, "freq").const_data_ptr();
+            rot = sizes_to_int(2 * half[0], "freq");
+        }
+        const int norm = PyObject_IsTrue(a[4]), paired = PyObject_IsTrue(a[5]);
+        if (norm < 0 || paired < 0) throw PyError{};
+        flags = (norm ? GFWA_HEAD_NORM : 0) | (paired ? GFWA_ROPE_PAIRED : 0);
+        if (!norm && (wq != nullptr || wk != nullptr)) fail(PyExc_ValueError, "wq and wk are weights of the norm, which norm=False leaves out");
+    }
+};
+
+PyObject* none_or(Output* o) {
+    if (o == nullptr) Py_RETURN_NONE;
+    return o->object();
+}
+template <size_t N>
+PyObject* tuple_or_none(Output* const (&outs)[N]) {
+    PyObject* r = PyTuple_New((Py_ssize_t)N);
+    if (r == nullptr) throw PyError{};
+    for (size_t i = 0; i < N; ++i) {
+        PyObject* x = none_or(outs[i]);
+        if (x == nullptr) {
+            Py_DECREF(r);
+            throw PyError{};
+        }
+        PyTuple_SET_ITEM(r, (Py_ssize_t)i, x);
+    }
+    return r;
+}
+
+PyObject* qk_norm_rope(PyObject* const* a) {  // q, k, v, wq, wk, eps, freq, norm, paired, pos, Q, K, V
+    const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
+    if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d]");
+    const int64_t B = q.size(0), N = q.size(1), H = q.size(2), d = q.size(3), Hkv = kv_heads(H, k.size(2));
+    const int dt = storage_type(q);
+    const at::ScalarType st = q.scalar_type();
+    const OneDevice dev(q);
+    const int64_t qs[4] = {B, N, H, d}, ks[4] = {B, N, Hkv, d}, Qs[4] = {B, H, N, d}, Ks[4] = {B, Hkv, N, d}, ps[2] = {B, N};
+    const Heads hq(q, qs, st, dev, "q", false), hk(k, ks, st, dev, "k", false);
+    const Heads hv = a[2] == Py_None ? Heads() : Heads(tensor_of(a[2], "v"), ks, st, dev, "v", false);
+    const Rotation how(a + 3, d, dev);
+    const void* pos = optional_input(a[9], ps, at::kInt, dev, "pos");
+    for (int i = 10; i < 13; ++i)
+        if (a[i] != Py_None) dev.also(tensor_of(a[i], "an output"), "an output");
+    dev.is_current();
+    Output Q(a[10], Qs, st, q.device(), "Q"), K(a[11], Ks, st, q.device(), "K");
+    std::optional<Output> V;
+    if (hv.given) V.emplace(a[12], Ks, st, q.device(), "V");
+    call([&] {
+        return lib.qk_norm_rope(dt, hq.get(), hk.get(), hv.get(), how.wq, how.wk, how.eps, how.freq, how.rot, (const int*)pos, how.flags,
+                                Q.ptr, K.ptr, V ? V->ptr : nullptr, (int)B, (int)H, (int)Hkv, (int)N, (int)d, stream());
+    });
+    return tuple_or_none({&Q, &K, V ? &*V : nullptr});
+}
+
+// A gradient of heads: the caller's strided tensor, checked, or a fresh dense one.
+struct HeadsOutput {
+    std::optional<Output> made;
+    PyObject* given = nullptr;
+    Heads h;
+    HeadsOutput(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const OneDevice& dev, const char* name) {
+        if (o == Py_None) {
+            made.emplace(o, shape, dtype, dev.device, name);
+            h = Heads(made->made, shape, dtype, dev, name, true);
+        } else {
+            h = Heads(tensor_of(o, name), shape, dtype, dev, name, true);
+            given = o;
+        }
+    }
+    PyObject* object() {
+        if (made) return made->object();
+        Py_INCREF(given);
+        return given;
+    }
+};
+
+// q, k, dQ, dK, dV, wq, wk, eps, freq, norm, paired, pos, dq, dk, dv, dwq, dwk, workspace
+PyObject* qk_norm_rope_backward(PyObject* const* a) {
+    const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
+    if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d]");
+    const int64_t B = q.size(0), N = q.size(1), H = q.size(2), d = q.size(3), Hkv = kv_heads(H, k.size(2));
+    const int dt = storage_type(q);
+    const at::ScalarType st = q.scalar_type();
+    const OneDevice dev(q);
+    const int64_t qs[4] = {B, N, H, d}, ks[4] = {B, N, Hkv, d}, Qs[4] = {B, H, N, d}, Ks[4] = {B, Hkv, N, d}, ps[2] = {B, N}, ws[1] = {d};
+    const Heads hq(q, qs, st, dev, "q", false), hk(k, ks, st, dev, "k", false);
+    const void *dQ = dense(a[2], Qs, st, dev, "dQ").const_data_ptr(), *dK = dense(a[3], Ks, st, dev, "dK").const_data_ptr();
+    const void* dV = optional_input(a[4], Ks, st, dev, "dV");
+    const Rotation how(a + 5, d, dev);
+    const void* pos = optional_input(a[11], ps, at::kInt, dev, "pos");
+    for (int i = 15; i < 18; ++i)
+        if (a[i] != Py_None) dev.also(tensor_of(a[i], "an output"), "an output");
+    const bool wants[2] = {how.wq != nullptr || a[15] != Py_None, how.wk != nullptr || a[16] != Py_None};
+    if (!(how.flags & GFWA_HEAD_NORM) && (wants[0] || wants[1])) fail(PyExc_ValueError, "dwq and dwk belong to the norm, which norm=False leaves out");
+    if (dV == nullptr && a[14] != Py_None) fail(PyExc_ValueError, "dv without dV");
+    dev.is_current();
+    HeadsOutput dq(a[12], qs, st, dev, "dq"), dk(a[13], ks, st, dev, "dk");
+    std::optional<HeadsOutput> dv;
+    if (dV != nullptr) dv.emplace(a[14], ks, st, dev, "dv");
+    std::optional<Output> dw[2];
+    for (int i = 0; i < 2; ++i)
+        if (wants[i]) dw[i].emplace(a[15 + i], ws, at::kFloat, dev.device, i ? "dwk" : "dwq");
+    std::optional<Workspace> scratch;
+    if (wants[0] || wants[1])
+        scratch.emplace(a[17], a[17] == Py_None ? lib.qk_norm_rope_backward_workspace_bytes((int)B, (int)H, (int)Hkv, (int)N, (int)d) : 0, dev.device);
+    call([&] {
+        return lib.qk_norm_rope_backward(dt, hq.get(), hk.get(), how.wq, how.wk, how.eps, how.freq, how.rot, (const int*)pos, how.flags, dQ, dK, dV,
+                                         dq.h.get(), dk.h.get(), dv ? dv->h.get() : nullptr, dw[0] ? (float*)dw[0]->ptr : nullptr,
+                                         dw[1] ? (float*)dw[1]->ptr : nullptr, scratch ? scratch->ptr : nullptr, scratch ? scratch->bytes : 0,
+                                         (int)B, (int)H, (int)Hkv, (int)N, (int)d, stream());
+    });
+    PyObject* out[5] = {dq.object(), dk.object(), dv ? dv->object() : none_or(nullptr), none_or(dw[0] ? &*dw[0] : nullptr),
+                        none_or(dw[1] ? &*dw[1] : nullptr)};
+    PyObject* r = PyTuple_New(5);
+    for (int i = 0; i < 5; ++i) {
+        if (r == nullptr || out[i] == nullptr) {
+            for (int k2 = i; k2 < 5; ++k2) Py_XDECREF(out[k2]);
+            Py_XDECREF(r);
+            throw PyError{};
+        }
+        PyTuple_SET_ITEM(r, i, out[i]);
+    }
+    return r;
+}
+
+// the paged cache both calls take: Kp, Vp [pages,Hkv,page,d], cp [pages,H,page] or None, table [B,max_pages]
+struct Pages {
+    int64_t pages, page, max_pages;
+    void *Kp, *Vp;
+    float* cp = nullptr;
+    const int* table;
+    Pages(PyObject* K, PyObject* V, PyObject* c, PyObject* t, int64_t B, int64_t H, int64_t Hkv, int64_t d, at::ScalarType st, const OneDevice& dev,
+          bool write) {
+        const at::Tensor& k = tensor_of(K, "Kp");
+        const at::Tensor& tab = tensor_of(t, "table");
+        if (k.dim() != 4 || tab.dim() != 2) fail(PyExc_ValueError, "Kp must be [pages,Hkv,page,d] and table [B,max_pages]");
+        pages = k.size(0);
+        page = k.size(2);
+        max_pages = tab.size(1);
+        const int64_t ks[4] = {pages, Hkv, page, d}, cs[3] = {pages, H, page}, ts[2] = {B, max_pages};
+        const at::Tensor& kt = dense(K, ks, st, dev, "Kp");
+        const at::Tensor& vt = dense(V, ks, st, dev, "Vp");
+        Kp = write ? kt.data_ptr() : const_cast<void*>(kt.const_data_ptr());
+        Vp = write ? vt.data_ptr() : const_cast<void*>(vt.const_data_ptr());
+        if (c != Py_None) {
+            const at::Tensor& ct = dense(c, cs, at::kFloat, dev, "cp");
+            cp = (float*)(write ? ct.data_ptr() : const_cast<void*>(ct.const_data_ptr()));
+        }
+        table = (const int*)dense(t, ts, at::kInt, dev, "table").const_data_ptr();
+        sizes_to_int(pages, "the number of pages");
+        sizes_to_int(page, "the page");
+        sizes_to_int(max_pages, "the table");
+    }
+};
+
+// k, v, Kp, Vp, start, cached, table, q, wq, wk, eps, freq, norm, paired, alpha, cp, Q
+PyObject* append_paged(PyObject* const* a) {
+    const at::Tensor& k = tensor_of(a[0], "k");
+    if (k.dim() != 3) fail(PyExc_ValueError, "k must be [rows,Hkv,d]");
+    const int64_t rows = k.size(0), Hkv = k.size(1), d = k.size(2);
+    int64_t H = Hkv;
+    const bool gated = a[14] != Py_None;
+    if (a[7] != Py_None) {
+        const at::Tensor& q = tensor_of(a[7], "q");
+        if (q.dim() != 3) fail(PyExc_ValueError, "q must be [rows,H,d]");
+        H = q.size(1);
+    } else if (gated) {
+        const at::Tensor& al = tensor_of(a[14], "alpha");
+        if (al.dim() != 2) fail(PyExc_ValueError, "alpha must be [rows,H]");
+        H = al.size(1);
+    }
+    kv_heads(H, Hkv);
+    const int dt = storage_type(k);
+    const at::ScalarType st = k.scalar_type();
+    const OneDevice dev(k);
+    const at::Tensor& cached = tensor_of(a[5], "cached");
+    if (cached.dim() != 1) fail(PyExc_ValueError, "cached must be [B]");
+    const int64_t B = cached.size(0), qs[3] = {rows, H, d}, ks[3] = {rows, Hkv, d}, bs[1] = {B}, ss[1] = {B + 1}, as[2] = {rows, H};
+    const Heads hk(k, ks, st, dev, "k", false), hv(tensor_of(a[1], "v"), ks, st, dev, "v", false);
+    const Heads hq = a[7] == Py_None ? Heads() : Heads(tensor_of(a[7], "q"), qs, st, dev, "q", false);
+    const void *start = dense(a[4], ss, at::kInt, dev, "start").const_data_ptr(), *before = dense(a[5], bs, at::kInt, dev, "cached").const_data_ptr();
+    const Rotation how(a + 8, d, dev);
+    const float* alpha = nullptr;
+    int64_t alpha_token = 0, alpha_head = 0;
+    if (gated) {
+        const at::Tensor& al = tensor_of(a[14], "alpha");
+        if (!al.is_cuda()) fail(PyExc_ValueError, "alpha must live on the GPU");
+        if (al.sizes() != at::IntArrayRef(as))
+            fail(PyExc_ValueError, "alpha has shape " + shape_text(al.sizes()) + ", expected " + shape_text(as));
+        if (al.scalar_type() != at::kFloat) fail(PyExc_TypeError, "alpha has dtype " + dtype_text(al.scalar_type()) + ", expected torch.float32");
+        dev.also(al, "alpha");
+        alpha = (const float*)al.const_data_ptr();
+        alpha_token = rows > 1 ? al.stride(0) : 0;
+        alpha_head = H > 1 ? al.stride(1) : 0;
+        if (a[15] == Py_None) fail(PyExc_ValueError, "alpha without cp");
+    }
+    const Pages cache(a[2], a[3], gated ? a[15] : Py_None, a[6], B, H, Hkv, d, st, dev, true);
+    if (a[16] != Py_None) dev.also(tensor_of(a[16], "Q"), "Q");
+    dev.is_current();
+    std::optional<Output> Q;
+    if (hq.given) Q.emplace(a[16], qs, st, dev.device, "Q");
+    call([&] {
+        return lib.append_paged(dt, hq.get(), hk.get(), hv.get(), how.wq, how.wk, how.eps, how.freq, how.rot, how.flags, alpha, alpha_token,
+                                alpha_head, (const int*)start, (const int*)before, cache.table, Q ? Q->ptr : nullptr, cache.Kp, cache.Vp, cache.cp,
+                                sizes_to_int(rows, "rows"), (int)B, (int)H, (int)Hkv, (int)d, (int)cache.pages, (int)cache.page, (int)cache.max_pages,
+                                stream());
+    });
+    return none_or(Q ? &*Q : nullptr);
+}
+
+PyObject* decode_paged(PyObject* const* a) {  // q, Kp, Vp, cp, table, pos, w, scale, o, L, workspace
+    const at::Tensor& q = tensor_of(a[0], "q");
+    const at::Tensor& k = tensor_of(a[1], "Kp");
+    if (q.dim() != 3 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,H,d] and Kp [pages,Hkv,page,d]");
+    const int64_t B = q.size(0), H = q.size(1), d = q.size(2), Hkv = kv_heads(H, k.size(1)), qs[3] = {B, H, d}, heads[2] = {B, H}, bs[1] = {B};
+    const int dt = storage_type(q);
+    const OneDevice dev(q);
+    need(q, qs, q.scalar_type(), "q");
+    if (a[3] == Py_None) fail(PyExc_TypeError, "cp must be a tensor");
+    const Pages cache(a[1], a[2], a[3], a[4], B, H, Hkv, d, q.scalar_type(), dev, false);
+    const void* pos = dense(a[5], bs, at::kInt, dev, "pos").const_data_ptr();
+    const int w = as_int(a[6]);
+    const float scale = as_float(a[7]);
+    for (int i = 8; i < 11; ++i)
+        if (a[i] != Py_None) dev.also(tensor_of(a[i], "an output"), "an output");
+    dev.is_current();
+    Output o(a[8], qs, q.scalar_type(), dev.device, "o"), L(a[9], heads, at::kFloat, dev.device, "L");
+    Workspace ws(a[10], a[10] == Py_None ? lib.decode_paged_workspace_bytes((int)B, (int)H, (int)Hkv, (int)d, (int)cache.page, (int)cache.max_pages, w) : 0,
+                 dev.device);
+    call([&] {
+        return lib.decode_paged(dt, q.const_data_ptr(), cache.Kp, cache.Vp, cache.cp, cache.table, (const int*)pos, o.ptr, (float*)L.ptr, ws.ptr,
+                                ws.bytes, (int)B, (int)H, (int)Hkv, (int)d, (int)cache.pages, (int)cache.page, (int)cache.max_pages, w, scale,
+                                stream());
+    });
+    return tuple_of({&o, &L});
+}
+
 // bind(check, (address, ...)): binding._check and the functions of `Library`, in its order
 PyObject* bind(PyObject* const* a) {
     if (!PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != kFunctions)
@@ -430,6 +744,10 @@ PyMethodDef methods[] = {GFWA_ENTRY(bind, 2),
                          GFWA_ENTRY(backward, 15),
                          GFWA_ENTRY(decode, 11),
                          GFWA_ENTRY(decode_static, 10),
+                         GFWA_ENTRY(qk_norm_rope, 13),
+                         GFWA_ENTRY(qk_norm_rope_backward, 18),
+                         GFWA_ENTRY(append_paged, 17),
+                         GFWA_ENTRY(decode_paged, 11),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gfwa_call", "Checked calls of libgfwa on torch tensors.", -1, methods};
 

@@ -86,6 +86,41 @@ hipError_t decode(bool bf16, const void* q, const void* Kc, const void* Vc, floa
 constexpr size_t kDecodeStaticBytes = (size_t)32 << 20;
 hipError_t decode_static_scratch(float** ptr);
 
+// ---- around the attention (include/gfwa_layer.h)
+// A strided tensor of heads: element e of head h of token n of sequence b at data + b * batch + n * token + h * head + e.
+struct HeadsView {
+    void* data;
+    long long batch, token, head;
+};
+struct HeadRotation {  // norm and rotation of queries and keys, as the entry points take them
+    const float *wq, *wk;
+    float eps;
+    const double* freq;
+    int rot;
+    const int* pos;
+    bool norm, paired;
+};
+hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const HeadsView& v, const HeadRotation& how, void* Q, void* K, void* V,
+                        int B, int H, int Hkv, int N, int d, hipStream_t s);
+size_t qk_norm_rope_backward_workspace_bytes(int d);
+// part: qk_norm_rope_backward_workspace_bytes() of scratch, used where dwq or dwk is given.
+hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView& k, const HeadRotation& how, const void* dQ, const void* dK,
+                                 const void* dV, const HeadsView& dq, const HeadsView& dk, const HeadsView& dv, float* dwq, float* dwk, float* part,
+                                 int B, int H, int Hkv, int N, int d, hipStream_t s);
+// A paged cache: Kp, Vp [pages,Hkv,page,d], cp [pages,H,page]; table [B,max_pages].
+struct PagedCache {
+    void *Kp, *Vp;
+    float* cp;
+    const int* table;
+    int pages, page, max_pages;
+};
+hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const HeadsView& v, const HeadRotation& how, const float* alpha,
+                        long long alpha_token, long long alpha_head, const int* start, const int* cached, void* Q, const PagedCache& cache, int rows,
+                        int B, int H, int Hkv, int d, hipStream_t s);
+size_t decode_paged_workspace_bytes(int B, int H, int Hkv, int d, int page, int max_pages, int w);
+hipError_t decode_paged(bool bf16, const void* q, const PagedCache& cache, const int* pos, void* o, float* L, float* part, int B, int H, int Hkv,
+                        int d, int w, float scale, hipStream_t s);
+
 // Calibration kernels (probe.hip): a pure bf16 MFMA loop and a plain 16-byte copy.
 hipError_t probe_mfma(float* sink, int iterations, int workgroups, int random_operands, double* flops, hipStream_t s);
 hipError_t probe_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
@@ -93,7 +128,9 @@ hipError_t probe_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 // Kernel ids for the optional per-kernel event timing (see gfwa_profile_* in include/gfwa.h).
 enum KernelId { kKernGatePrefix = 0, kKernForward, kKernRowDot, kKernDkv, kKernDq, kKernGateGrad, kKernGateActPrefix,
                 kKernGateActBwd, kKernDecode, kKernDecodeCombine, kKernScanSegmentSum,
-                kKernScanPropagate, kKernGateGradSegmentSum, kKernCount };
+                kKernScanPropagate, kKernGateGradSegmentSum, kKernNormRope, kKernNormRopeBwd, kKernNormWeightSum, kKernAppendPaged,
+                kKernDecodePaged, kKernDecodePagedCombine, kKernCount };
+constexpr int kKernFirstCount = 13;  // ids there were when gfwa_profile_read was defined: callers may ask for these alone
 
 // Per-device launch set-up, done once per device and kernel (`done`: one bit per device id, owned by the caller):
 // lets `kernel` use `bytes` of dynamic LDS on the current device.
