@@ -26,6 +26,7 @@ struct AppendArgs {
     float* cp;
     int rows, B, H, Hkv, pages, page, max_pages;
     int scan_blocks;   // workgroups of the prefix, in front
+    int scan_heads;    // heads that a wave of them takes: 8, or 1
     long long items;   // row tiles x head ranges
     int ranges, heads;
 };
@@ -39,8 +40,11 @@ __device__ __forceinline__ int page_of(const AppendArgs& a, int b, long long p, 
     return id >= 0 && id < a.pages ? id : -1;
 }
 
-// The sequence b with start[b] <= row < start[b + 1], or -1.
+// The sequence b with start[b] <= row < start[b + 1], or -1.  In a decoding step row b is sequence b's: that guess takes one round of
+// loads where the search takes one for each halving of the batch.
 __device__ __forceinline__ int sequence_of(const int* start, int B, int row) {
+    const int guess = min(row, B - 1);
+    if (start[guess] <= row && row < start[guess + 1]) return guess;
     int lo = 0, hi = B;
     while (hi - lo > 1) {
         const int mid = lo + (hi - lo) / 2;
@@ -50,27 +54,113 @@ __device__ __forceinline__ int sequence_of(const int* start, int B, int row) {
     return start[lo] <= row && row < start[lo + 1] ? lo : -1;
 }
 
-// c_p of every new token of sequence b and head h, by one thread.
-__device__ void prefix_of(const AppendArgs& a, int b, int h) {
-    const int n0 = min(max(a.start[b], 0), a.rows), n1 = min(max(a.start[b + 1], n0), a.rows);
-    const long long before = a.cached[b];
-    double c = 0;
-    int row = 0;
-    const int prev = n1 > n0 ? page_of(a, b, before - 1, row) : -1;
-    if (prev >= 0) c = a.cp[((size_t)prev * a.H + h) * a.page + row];
-    for (int n = n0; n < n1; ++n) {
-        c += a.alpha[n * a.alpha_token + h * a.alpha_head];
-        const int id = page_of(a, b, before + (n - n0), row);
-        if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + row] = (float)c;
+// ---- the prefix: fp64 sums, each c rounded once
+
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double dpp_or_zero(double x) {  // lanes without a source, or in a row that ROWS leaves out, get 0
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    return __builtin_bit_cast(double, i32x2{__builtin_amdgcn_update_dpp(0, v[0], CTRL, ROWS, 0xf, false),
+                                            __builtin_amdgcn_update_dpp(0, v[1], CTRL, ROWS, 0xf, false)});
+}
+__device__ __forceinline__ double wave_scan(double x) {  // inclusive, over the 64 lanes
+    x += dpp_or_zero<0x111>(x);
+    x += dpp_or_zero<0x112>(x);
+    x += dpp_or_zero<0x114>(x);
+    x += dpp_or_zero<0x118>(x);
+    x += dpp_or_zero<0x142, 0xa>(x);
+    x += dpp_or_zero<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ double lane_value(double x, int lane) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    return __builtin_bit_cast(double, i32x2{__builtin_amdgcn_readlane(v[0], lane), __builtin_amdgcn_readlane(v[1], lane)});
+}
+
+constexpr int kShort = 8;       // new tokens, and heads, that a wave takes in one go
+constexpr int kScanGroups = 8;  // groups of 64 tokens of a pass over a long sequence
+
+// New tokens n0 .. n1 of sequence b, whose cache holds `before` tokens: c of one head, by one wave.  The gates and page ids of the next 512
+// tokens are on their way while these are added up.
+__device__ void prefix_long(const AppendArgs& a, int b, int h, int n0, int n1, long long before, double c) {
+    const int lane = threadIdx.x & 63;
+    const float* alpha = a.alpha + h * a.alpha_head;
+    float x[2][kScanGroups];
+    int id[2][kScanGroups];
+    auto issue = [&](int n, auto buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kScanGroups; ++u) {
+            const int t = n + 64 * u + lane;
+            x[decltype(buf)::value][u] = t < n1 ? alpha[t * a.alpha_token] : 0.f;
+            int row;
+            id[decltype(buf)::value][u] = t < n1 ? page_of(a, b, before + (t - n0), row) : -1;
+        }
+    };
+    auto add = [&](int n, auto buf) __attribute__((always_inline)) {
+        constexpr int k = decltype(buf)::value;
+#pragma unroll
+        for (int u = 0; u < kScanGroups; ++u) {
+            const double s = wave_scan((double)x[k][u]);
+            if (id[k][u] >= 0) {  // a position in the table: 32 bits
+                const int p = (int)(before + (n - n0)) + 64 * u + lane;
+                a.cp[((size_t)id[k][u] * a.H + h) * a.page + p % a.page] = (float)(c + s);
+            }
+            c += lane_value(s, 63);
+        }
+    };
+    constexpr int kPass = 64 * kScanGroups;
+    const std::integral_constant<int, 0> first;
+    const std::integral_constant<int, 1> second;
+    issue(n0, first);
+    for (int n = n0; n < n1; n += 2 * kPass) {
+        if (n1 - n > kPass) issue(n + kPass, second);
+        add(n, first);
+        if (n1 - n > kPass) {
+            if (n1 - n > 2 * kPass) issue(n + 2 * kPass, first);
+            add(n + kPass, second);
+        }
     }
+}
+
+// c of the new tokens of sequence b for `heads` (1 or 8) heads from h0 on, by one wave.  A few tokens and eight heads: a lane for each of both.
+__device__ void prefix_of(const AppendArgs& a, int b, int h0, int heads) {
+    const int lane = threadIdx.x & 63;
+    const int n0 = min(max(a.start[b], 0), a.rows), n1 = min(max(a.start[b + 1], n0), a.rows);
+    if (n0 == n1) return;
+    const long long before = a.cached[b];
+    int row = 0;
+    const int prev = page_of(a, b, before - 1, row);
+    auto cached_c = [&](int h) { return prev >= 0 ? (double)a.cp[((size_t)prev * a.H + h) * a.page + row] : 0.0; };
+    const int last = min(h0 + heads, a.H);
+    if (heads == kShort && n1 - n0 <= kShort) {
+        const int t = lane / kShort, h = h0 + lane % kShort;
+        const bool mine = n0 + t < n1 && h < last;
+        double c = mine ? a.alpha[(n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
+        if (n1 - n0 > 1) {
+#pragma unroll
+            for (int off = kShort; off < 64; off *= 2) {
+                const double x = __shfl_up(c, off, 64);
+                if (lane >= off) c += x;
+            }
+        }
+        if (!mine) return;
+        c += cached_c(h);
+        int to = 0;
+        const int id = page_of(a, b, before + t, to);
+        if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + to] = (float)c;
+        return;
+    }
+    for (int h = h0; h < last; ++h) prefix_long(a, b, h, n0, n1, before, cached_c(h));
 }
 
 template <typename T, int D>
 __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16, RPW = 64 / LPR;
     if ((int)blockIdx.x < a.scan_blocks) {
-        const long long i = (long long)blockIdx.x * (64 * kAppendWaves) + threadIdx.x;
-        if (i < (long long)a.B * a.H) prefix_of(a, (int)(i / a.H), (int)(i % a.H));
+        const long long i = (long long)blockIdx.x * kAppendWaves + (threadIdx.x >> 6);
+        const int units = (a.H + a.scan_heads - 1) / a.scan_heads;
+        if (i < (long long)a.B * units) prefix_of(a, (int)(i / units), (int)(i % units) * a.scan_heads, a.scan_heads);
         return;
     }
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
@@ -161,7 +251,11 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.page = cache.page;
     a.max_pages = cache.max_pages;
     constexpr int kThreads = 64 * kAppendWaves;
-    a.scan_blocks = alpha != nullptr ? (int)(((long long)B * H + kThreads - 1) / kThreads) : 0;
+    // a wave of the prefix takes one head where sequences bring many tokens (more than 16 on average: those with few leave
+    // its lanes idle, those with many are bound by it), eight where they bring few
+    a.scan_heads = rows > 16LL * B ? 1 : kShort;
+    const long long scans = (long long)B * ((H + a.scan_heads - 1) / a.scan_heads);
+    a.scan_blocks = alpha != nullptr ? (int)((scans + kAppendWaves - 1) / kAppendWaves) : 0;
     const int heads = H + 2 * Hkv;
     const long long tiles = (rows + 1024 / d - 1) / (1024 / d), waves = 16LL * device_cu_count();
     long long ranges = (waves + tiles - 1) / tiles;
