@@ -12,7 +12,8 @@ namespace {
 
 constexpr int kUnit = 16;       // positions of a unit; pages are multiples of it
 constexpr int kChunkUnits = 16; // a chunk of the window is a multiple of this many units
-constexpr int kTileWaves = 4;   // waves of a workgroup on the matrix cores
+constexpr int kTileUnits = 2;  // bf16: units of a tile
+constexpr long long kOnceBytes = 24 << 20;  // windows of more than this are loaded past the caches: the L2s hold 32 MiB
 constexpr float kNone = -1.0e30f;
 
 // Partial result of one (query head, chunk): D output columns (not yet divided by the sum), the exponent they are scaled
@@ -28,6 +29,7 @@ struct PagedArgs {
     int H, Hkv, pages, page, max_pages, w;
     float scale;
     int splits, chunk;  // chunks of the window and units (bf16: tiles) of one
+    int items;          // workgroups of one chunk
     int units_shift;    // log2 of the units of a page, -1: no power of two
 };
 
@@ -51,7 +53,7 @@ struct Query {
 //
 // A wave takes tiles of two units (32 keys), newest first, for up to 16 query heads of one key/value head:
 //   S  [16 keys x 16 heads] = K [16 x D] Q^T          for each unit; K straight from memory in the A operand's layout (row: lane % 16)
-//   O^T[D x 16 heads]      += V^T [D x 32 keys] P^T   P as it leaves S: lane (head, g) has the keys 4 g + 0..3 of both units, which is
+//   O^T[D x 16 heads]      += V^T [D x 32 keys] P^T   P as it leaves S: lane (head, g) has the keys 4 g + 0..3 of two units, which is
 //                                                     a B operand for a contraction over the keys in that order; V^T through LDS, which
 //                                                     hands out transposed pieces in the same order
 // Weights are rounded to bf16 on their way into the second product (half a step, 2^-8 of each, is what an output is rounded by too); their sum is
@@ -61,7 +63,7 @@ struct Query {
 // Loads of the next tile are on their way while a tile is worked on.
 template <int D>
 struct VTile {  // 32 keys of V in LDS, 16-byte chunks permuted so that neither the row-wise writes nor the transposed reads meet in a bank
-    static constexpr int kBytes = 32 * D * 2;
+    static constexpr int kBytes = kTileUnits * kUnit * D * 2;
     static __device__ __forceinline__ int off(int row, int chunk) {
         const int f = D == 128 ? ((row & 3) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1))
                                : (((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1));  // two rows share the banks' width
@@ -71,16 +73,18 @@ struct VTile {  // 32 keys of V in LDS, 16-byte chunks permuted so that neither 
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-template <int D, int NW>
+// ONCE: V is loaded past the caches.  No other workgroup reads it, and a window that the L2s do not hold is read faster (us, H 32, Hkv 8, d 128,
+// w 1024: 64 sequences 49.4 -> 46.0, 32 26.1 -> 22.8; H 32, Hkv 4, d 64, whole sequences of up to 16384 40.7 -> 33.8), one that they do hold more
+// slowly (2 sequences of H 16, d 64, w 512, 4 MB, 6.7 -> 7.2).  K's lines are asked for by two loads each: past the caches 47.6 for the first.
+template <int D, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void decode_paged_mfma_kernel(const PagedArgs a) {
-    constexpr int KS = D / 32, DT = D / 16, CPR = D / 8, RPI = 64 / CPR, VL = 32 / RPI;  // VL: loads of a lane for 32 rows of V
+    constexpr int KS = D / 32, DT = D / 16, CPR = D / 8, RPI = 64 / CPR, NU = kTileUnits, VU = kUnit / RPI;  // VU: loads of a lane for a unit of V
     constexpr int kHeads = 16, kPitch = D + 4;  // floats between the heads' sums when the waves merge
-    constexpr int kWave = VTile<D>::kBytes > kHeads * kPitch * 4 ? VTile<D>::kBytes : kHeads * kPitch * 4;
+    constexpr int kWave = kHeads * kPitch * 4 > VTile<D>::kBytes ? kHeads * kPitch * 4 : VTile<D>::kBytes;
     __shared__ __align__(16) char lds[NW * kWave];
     __shared__ float sm_m[NW][kHeads], sm_l[NW][kHeads];
-    int idx = blockIdx.x;
-    const int s = idx % a.splits;
-    idx /= a.splits;
+    const int s = blockIdx.x / a.items;  // the newest chunks of all come first, those that short sequences do not have last
+    int idx = (blockIdx.x - s * a.items + s) % a.items;  // a sequence's chunks on other XCDs
     const int G = a.H / a.Hkv, gchunks = (G + kHeads - 1) / kHeads, gc = idx % gchunks;
     idx /= gchunks;
     const int kvh = idx % a.Hkv, b = idx / a.Hkv;
@@ -97,7 +101,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_mfma_kernel(const Pag
 
     // the tiles of this chunk, counted from the newest unit back
     const int u_hi = me.p / kUnit, u_lo = me.lo / kUnit;
-    const int t1 = me.page < 0 ? 0 : min((s + 1) * a.chunk, (u_hi - u_lo) / 2 + 1);
+    const int t1 = me.page < 0 ? 0 : min((s + 1) * a.chunk, (u_hi - u_lo) / NU + 1);
+    if (a.splits > 1 && s * a.chunk >= t1) return;  // the merge knows
     int t = s * a.chunk + wv;
     if (t < t1) {
         const bf16_t* const K = (const bf16_t*)a.Kp + (size_t)kvh * a.page * D;
@@ -124,69 +129,77 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_mfma_kernel(const Pag
             if (id >= 0 && id < a.pages) x = Unit{id, u * kUnit - i * a.page, true};
             return x;
         };
-        bf16x8 kf[2][KS], vf[VL];
-        f32x4_any cf[2];
-        bool there[2];
+        bf16x8 kf[NU][KS], vf[NU][VU];
+        f32x4_any cf[NU];
+        bool there[NU];
+        Unit next[NU];
         const int vrow = lane / CPR, vcol = lane % CPR;
-        auto issue = [&](const Unit (&x)[2]) __attribute__((always_inline)) {
+        auto look_up = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                there[n] = x[n].there;
-                const size_t at = ((size_t)x[n].page * a.Hkv * a.page + x[n].row) * D;
+            for (int n = 0; n < NU; ++n) next[n] = unit(u_hi - NU * tile - n);
+        };
+        auto issue = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < NU; ++n) {
+                there[n] = next[n].there;
+                const size_t at = ((size_t)next[n].page * a.Hkv * a.page + next[n].row) * D;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) kf[n][k] = *reinterpret_cast<const bf16x8*>(K + at + hd * D + 32 * k + 8 * g);
-                cf[n] = *reinterpret_cast<const f32x4_any*>(C + (size_t)x[n].page * a.H * a.page + x[n].row + 4 * g);
+                cf[n] = *reinterpret_cast<const f32x4_any*>(C + (size_t)next[n].page * a.H * a.page + next[n].row + 4 * g);
 #pragma unroll
-                for (int i = 0; i < VL / 2; ++i)
-                    vf[n * (VL / 2) + i] = *reinterpret_cast<const bf16x8*>(V + at + (i * RPI + vrow) * D + 8 * vcol);
-            }
-        };
-        Unit next[2] = {unit(u_hi - 2 * t), unit(u_hi - 2 * t - 1)};
-        issue(next);
-        if (t + NW < t1) {
-            next[0] = unit(u_hi - 2 * (t + NW));
-            next[1] = unit(u_hi - 2 * (t + NW) - 1);
-        }
-        for (; t < t1; t += NW) {
-            const int key0 = (u_hi - 2 * t) * kUnit, key1 = key0 - kUnit;  // first keys of the two units
-            const bool whole = there[0] && there[1] && key1 >= me.lo && key0 + kUnit - 1 <= me.p;
-            if (!whole) {  // values of masked keys do not enter the product, whatever they are
-#pragma unroll
-                for (int i = 0; i < VL; ++i) {
-                    const int n = i / (VL / 2), key = (n ? key1 : key0) + (i % (VL / 2)) * RPI + vrow;
-                    if (!(there[n] && key >= me.lo && key <= me.p)) vf[i] = bf16x8{};
+                for (int i = 0; i < VU; ++i) {
+                    const bf16x8* const from = reinterpret_cast<const bf16x8*>(V + at + (i * RPI + vrow) * D + 8 * vcol);
+                    if constexpr (ONCE) vf[n][i] = __builtin_nontemporal_load(from);
+                    else vf[n][i] = *from;
                 }
             }
+        };
+        look_up(t);
+        issue();
+        if (t + NW < t1) look_up(t + NW);
+        for (; t < t1; t += NW) {
+            const int key0 = (u_hi - NU * t) * kUnit;  // first key of the newest unit
+            bool whole = key0 - (NU - 1) * kUnit >= me.lo && key0 + kUnit - 1 <= me.p, was[NU];
 #pragma unroll
-            for (int i = 0; i < VL; ++i) *reinterpret_cast<bf16x8*>(mine + VTile<D>::off(i * RPI + vrow, vcol)) = vf[i];
-            f32x4 sc[2];
+            for (int n = 0; n < NU; ++n) {
+                was[n] = there[n];
+                whole = whole && there[n];
+            }
+            if (!whole) {  // values of masked keys do not enter the product, whatever they are
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+                for (int n = 0; n < NU; ++n)
+#pragma unroll
+                    for (int i = 0; i < VU; ++i) {
+                        const int key = key0 - n * kUnit + i * RPI + vrow;
+                        if (!(there[n] && key >= me.lo && key <= me.p)) vf[n][i] = bf16x8{};
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NU; ++n)
+#pragma unroll
+                for (int i = 0; i < VU; ++i) *reinterpret_cast<bf16x8*>(mine + VTile<D>::off(n * kUnit + i * RPI + vrow, vcol)) = vf[n][i];
+            f32x4 sc[NU];
+            float bias[NU][4];
+#pragma unroll
+            for (int n = 0; n < NU; ++n) {
                 sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < KS; ++k) sc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[n][k], q[k], sc[n], 0, 0, 0);
-            }
-            float bias[2][4];
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) bias[n][e] = (cf[n][e] - c0) * kLog2e;
-            const bool was[2] = {there[0], there[1]};
+            }
             if (t + NW < t1) {
-                issue(next);
-                if (t + 2 * NW < t1) {
-                    next[0] = unit(u_hi - 2 * (t + 2 * NW));
-                    next[1] = unit(u_hi - 2 * (t + 2 * NW) - 1);
-                }
+                issue();
+                if (t + 2 * NW < t1) look_up(t + 2 * NW);
             }
             __builtin_amdgcn_sched_barrier(0);
             float top = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < NU; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float x = fmaf(sc[n][e], to_log2, bias[n][e]);
-                    const int key = (n ? key1 : key0) + 4 * g + e;
+                    const int key = key0 - n * kUnit + 4 * g + e;
                     if (!whole) x = was[n] && key >= me.lo && key <= me.p ? x : -INFINITY;
                     sc[n][e] = x;
                     top = fmaxf(top, x);
@@ -202,25 +215,26 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_mfma_kernel(const Pag
                 for (int i = 0; i < DT; ++i) acc[i] *= f;
                 sum *= f;
             }
-            bf16x8 pr;
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = fast_exp2(sc[n][e] - m);
-                    sum += x;
-                    pr[4 * n + e] = (bf16_t)x;
-                }
             asm volatile("" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                const int row = 4 * g + (hd >> 2), col = 16 * i + 4 * (hd & 3);
-                const char* const at = mine + (col & 7) * 2;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + VTile<D>::off(row, col >> 3)));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + VTile<D>::off(16 + row, col >> 3)));
-                typedef short s16x8 __attribute__((ext_vector_type(8)));
-                const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pr, acc[i], 0, 0, 0);
+            for (int n = 0; n < NU; n += 2) {
+                bf16x8 pr;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = fast_exp2(sc[n + e / 4][e % 4] - m);
+                    sum += x;
+                    pr[e] = (bf16_t)x;
+                }
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    const int row = n * kUnit + 4 * g + (hd >> 2), col = 16 * i + 4 * (hd & 3);
+                    const char* const at = mine + (col & 7) * 2;
+                    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + VTile<D>::off(row, col >> 3)));
+                    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + VTile<D>::off(kUnit + row, col >> 3)));
+                    typedef short s16x8 __attribute__((ext_vector_type(8)));
+                    const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), pr, acc[i], 0, 0, 0);
+                }
             }
             asm volatile("" ::: "memory");
         }
@@ -275,9 +289,8 @@ __global__ __launch_bounds__(256) void decode_paged_kernel(const PagedArgs a) {
     constexpr int LPR = D / 8, RPI = 64 / LPR, NW = 4;
     __shared__ __align__(16) float sm_acc[NW][GT][D];
     __shared__ float sm_m[NW][GT], sm_l[NW][GT];
-    int idx = blockIdx.x;
-    const int s = idx % a.splits;
-    idx /= a.splits;
+    const int s = blockIdx.x / a.items;
+    int idx = (blockIdx.x - s * a.items + s) % a.items;
     const int G = a.H / a.Hkv, gchunks = G / GT, gc = idx % gchunks;
     idx /= gchunks;
     const int kvh = idx % a.Hkv, b = idx / a.Hkv;
@@ -293,6 +306,7 @@ __global__ __launch_bounds__(256) void decode_paged_kernel(const PagedArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[g][e] = 0.f;
     }
+    if (a.splits > 1 && (me.page < 0 || s * a.chunk > me.p / kUnit - me.lo / kUnit)) return;  // the merge knows
     if (me.page >= 0) {
         float q[GT][8], c0[GT];
 #pragma unroll
@@ -384,21 +398,63 @@ __global__ __launch_bounds__(256) void decode_paged_kernel(const PagedArgs a) {
 }
 
 // o = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  L = (M + log2 of that sum) ln 2
-template <typename T, int D>
-__global__ __launch_bounds__(D) void decode_paged_combine_kernel(const float* __restrict__ part, T* __restrict__ o, float* __restrict__ L, int S) {
+// over the chunks that hold part of the window (the others write nothing).  NG groups of D threads take every NG-th record each.
+template <typename T, int D, int NG>
+__global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const PagedArgs a) {
+    __shared__ float sm_o[NG][D], sm_m[NG], sm_l[NG];
     const size_t bh = blockIdx.x;
-    const int col = threadIdx.x;
-    const float* rec = part + bh * S * record(D);
+    const int col = threadIdx.x % D, grp = threadIdx.x / D;
+    const Query me(a, (int)(bh / a.H));
+    const int pieces = me.page < 0 ? 0 : (me.p / kUnit - me.lo / kUnit) / (sizeof(T) == 2 ? kTileUnits : 1) + 1;
+    const int there = (pieces + a.chunk - 1) / a.chunk;
+    const float* rec = a.part + bh * a.splits * record(D);
     float mm = kNone, ll = 0.f, oo = 0.f;
-    for (int s = 0; s < S; ++s) {
-        const float* x = rec + (size_t)s * record(D);
-        const float mn = fmaxf(mm, x[D]), f0 = fast_exp2(mm - mn), f = fast_exp2(x[D] - mn);
-        ll = ll * f0 + x[D + 1] * f;
-        oo = oo * f0 + x[col] * f;
+    constexpr int U = 8;  // records whose loads are in flight together
+    for (int s0 = grp; s0 < there; s0 += U * NG) {
+        float m[U], l[U], x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float* r = rec + (size_t)min(s0 + u * NG, there - 1) * record(D);
+            m[u] = r[D];
+            l[u] = s0 + u * NG < there ? r[D + 1] : 0.f;
+            x[u] = r[col];
+        }
+        float mn = mm;
+#pragma unroll
+        for (int u = 0; u < U; ++u) mn = fmaxf(mn, m[u]);
+        const float f0 = fast_exp2(mm - mn);
+        ll *= f0;
+        oo *= f0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = s0 + u * NG < there ? fast_exp2(m[u] - mn) : 0.f;
+            ll = fmaf(l[u], f, ll);
+            oo = fmaf(x[u], f, oo);
+        }
         mm = mn;
     }
-    o[bh * D + col] = (T)(ll == 0.f ? 0.f : oo / ll);
-    if (L != nullptr && col == 0) L[bh] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    if (NG > 1) {
+        sm_o[grp][col] = oo;
+        if (col == 0) {
+            sm_m[grp] = mm;
+            sm_l[grp] = ll;
+        }
+        __syncthreads();
+        if (grp > 0) return;
+        float mn = mm;
+#pragma unroll
+        for (int k = 1; k < NG; ++k) mn = fmaxf(mn, sm_m[k]);
+        ll = oo = 0.f;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const float f = fast_exp2(sm_m[k] - mn);
+            ll = fmaf(sm_l[k], f, ll);
+            oo = fmaf(sm_o[k][col], f, oo);
+        }
+        mm = mn;
+    }
+    ((T*)a.o)[bh * D + col] = (T)(ll == 0.f ? 0.f : oo / ll);
+    if (a.L != nullptr && col == 0) a.L[bh] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
 }
 
 // Units a window may touch, and the most chunks it is cut into.
@@ -410,17 +466,32 @@ int most_units(int page, int max_pages, int w) {
 
 // How a step is cut up; follows from the sizes alone, as the workspace does.
 struct Plan {
-    int GT, chunk, splits;  // query heads of a workgroup, units (bf16: tiles) of a chunk, chunks
+    int GT, waves;          // query heads (fp32) and waves of a workgroup
+    int chunk, splits;      // units (bf16: tiles) of a chunk, chunks
     long long items;        // workgroups of one chunk
-    Plan(bool bf16, int B, int H, int Hkv, int page, int max_pages, int w) {
+    Plan(bool bf16, int B, int H, int Hkv, int d, int page, int max_pages, int w) {
         const int G = H / Hkv, units = most_units(page, max_pages, w);
+        waves = 4;
         if (bf16) {
-            const int tiles = units / 2 + 1;
-            GT = 16;
+            const int tiles = (units + kTileUnits - 1) / kTileUnits;
             items = (long long)B * Hkv * ((G + 15) / 16);
-            long long S = (512 + items - 1) / items;  // two workgroups of four waves for each compute unit
-            if (S > (tiles + kTileWaves - 1) / kTileWaves) S = (tiles + kTileWaves - 1) / kTileWaves;
-            chunk = (int)(((tiles + S - 1) / S + kTileWaves - 1) / kTileWaves * kTileWaves);
+            // Measured (us, four and eight waves, graphs of 21 steps; H 32, Hkv 8, d 128 unless named):
+            //   * a window shorter than the table is about as long for every sequence.  Where one chunk each gives every compute unit two
+            //     workgroups of four waves that is best (64 sequences, w 1024: one chunk 49, two 54); with half of that, one of eight
+            //     waves (32 sequences: 26; two chunks of four waves 29); with fewer, chunks for two workgroups (8: 11.8, for one 13.0).
+            //   * whole sequences are of any length: chunks of two tiles a wave, or as many as make 4096 workgroups, level that (16 of up
+            //     to 8192: 70; 512 workgroups 79; H 32, Hkv 4, d 64, up to 16384: 41 and 53).
+            //   * a window of three tiles a wave is not worth the merge (300 keys of one sequence: 4.4, in three chunks 6.3).
+            const bool even = w < (long long)max_pages * page;
+            long long S = 1;
+            if (even && items >= 512) waves = 4;
+            else if (tiles <= 24 || (even && items >= 256)) waves = 8;
+            else {
+                const long long want = even ? 512 : 4096, least = even ? waves : 2 * waves;
+                S = (want + items - 1) / items;
+                if (S > (tiles + least - 1) / least) S = (tiles + least - 1) / least;
+            }
+            chunk = (int)(((tiles + S - 1) / S + waves - 1) / waves * waves);
             splits = (tiles + chunk - 1) / chunk;
             return;
         }
@@ -435,7 +506,7 @@ struct Plan {
 }  // namespace
 
 size_t decode_paged_workspace_bytes(int B, int H, int Hkv, int d, int page, int max_pages, int w) {
-    const int f32 = Plan(false, B, H, Hkv, page, max_pages, w).splits, bf16 = Plan(true, B, H, Hkv, page, max_pages, w).splits;
+    const int f32 = Plan(false, B, H, Hkv, d, page, max_pages, w).splits, bf16 = Plan(true, B, H, Hkv, d, page, max_pages, w).splits;
     return (size_t)B * H * (f32 > bf16 ? f32 : bf16) * record(d) * sizeof(float);
 }
 
@@ -443,18 +514,25 @@ template <typename T, int D>
 static hipError_t launch(const PagedArgs& given, int B, hipStream_t s) {
     PagedArgs a = given;
     constexpr bool kShort = sizeof(T) == 2;
-    const Plan plan(kShort, B, a.H, a.Hkv, a.page, a.max_pages, a.w);
+    const Plan plan(kShort, B, a.H, a.Hkv, D, a.page, a.max_pages, a.w);
     a.chunk = plan.chunk;
     a.splits = plan.splits;
+    a.items = (int)plan.items;
     {
         ProfScope prof(kKernDecodePaged, s);
         auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.items * a.splits)), dim3(threads), 0, s, a); };
-        if constexpr (kShort) go(decode_paged_mfma_kernel<D, kTileWaves>, 64 * kTileWaves);
+        if constexpr (kShort) {
+            const long long keys = (long long)a.max_pages * a.page, span = a.w < keys ? a.w : keys;
+            const bool once = plan.items == (long long)B * a.Hkv && plan.items * span * D * 2 * (long long)sizeof(T) > kOnceBytes;
+            if (plan.waves == 8) once ? go(decode_paged_mfma_kernel<D, 8, true>, 512) : go(decode_paged_mfma_kernel<D, 8, false>, 512);
+            else once ? go(decode_paged_mfma_kernel<D, 4, true>, 256) : go(decode_paged_mfma_kernel<D, 4, false>, 256);
+        }
         else plan.GT == 4 ? go(decode_paged_kernel<T, D, 4>, 256) : plan.GT == 2 ? go(decode_paged_kernel<T, D, 2>, 256) : go(decode_paged_kernel<T, D, 1>, 256);
     }
     if (a.splits > 1) {
         ProfScope prof(kKernDecodePagedCombine, s);
-        hipLaunchKernelGGL((decode_paged_combine_kernel<T, D>), dim3(B * a.H), dim3(D), 0, s, a.part, (T*)a.o, a.L, a.splits);
+        if (a.splits > 16) hipLaunchKernelGGL((decode_paged_combine_kernel<T, D, 4>), dim3(B * a.H), dim3(4 * D), 0, s, a);
+        else hipLaunchKernelGGL((decode_paged_combine_kernel<T, D, 1>), dim3(B * a.H), dim3(D), 0, s, a);
     }
     return hipGetLastError();
 }
