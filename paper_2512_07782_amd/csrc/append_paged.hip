@@ -27,8 +27,7 @@ struct AppendArgs {
     int rows, B, H, Hkv, pages, page, max_pages;
     int scan_blocks;   // workgroups of the prefix, in front
     int scan_heads;    // heads that a wave of them takes: 8, or 1
-    long long items;   // row tiles x head ranges
-    int ranges, heads;
+    Shares shares;     // of tiles of 1024 / D rows
 };
 
 // The page that holds position p of sequence b, or -1: outside the table, or not there.
@@ -40,18 +39,22 @@ __device__ __forceinline__ int page_of(const AppendArgs& a, int b, long long p, 
     return id >= 0 && id < a.pages ? id : -1;
 }
 
-// The sequence b with start[b] <= row < start[b + 1], or -1.  In a decoding step row b is sequence b's: that guess takes one round of
-// loads where the search takes one for each halving of the batch.
-__device__ __forceinline__ int sequence_of(const int* start, int B, int row) {
-    const int guess = min(row, B - 1);
-    if (start[guess] <= row && row < start[guess + 1]) return guess;
-    int lo = 0, hi = B;
+// The sequence b with start[b] <= row < start[b + 1], or -1, its first row and its tokens in the cache.  In a decoding step row b is sequence b's: that
+// guess takes one round of loads where the search takes one for each halving of the batch.
+__device__ __forceinline__ int sequence_of(const AppendArgs& a, int row, int& first, int& before) {
+    const int guess = min(row, a.B - 1), next = a.start[guess + 1];
+    first = a.start[guess];
+    before = a.cached[guess];
+    if ((first <= row) & (row < next)) return guess;
+    int lo = 0, hi = a.B;
     while (hi - lo > 1) {
         const int mid = lo + (hi - lo) / 2;
-        if (start[mid] <= row) lo = mid;
+        if (a.start[mid] <= row) lo = mid;
         else hi = mid;
     }
-    return start[lo] <= row && row < start[lo + 1] ? lo : -1;
+    first = a.start[lo];
+    before = a.cached[lo];
+    return first <= row && row < a.start[lo + 1] ? lo : -1;
 }
 
 // ---- the prefix: fp64 sums, each c rounded once
@@ -126,9 +129,10 @@ __device__ void prefix_long(const AppendArgs& a, int b, int h, int n0, int n1, l
 // c of the new tokens of sequence b for `heads` (1 or 8) heads from h0 on, by one wave.  A few tokens and eight heads: a lane for each of both.
 __device__ void prefix_of(const AppendArgs& a, int b, int h0, int heads) {
     const int lane = threadIdx.x & 63;
-    const int n0 = min(max(a.start[b], 0), a.rows), n1 = min(max(a.start[b + 1], n0), a.rows);
-    if (n0 == n1) return;
+    const int from = a.start[b], to = a.start[b + 1];
     const long long before = a.cached[b];
+    const int n0 = min(max(from, 0), a.rows), n1 = min(max(to, n0), a.rows);
+    if (n0 == n1) return;
     int row = 0;
     const int prev = page_of(a, b, before - 1, row);
     auto cached_c = [&](int h) { return prev >= 0 ? (double)a.cp[((size_t)prev * a.H + h) * a.page + row] : 0.0; };
@@ -136,6 +140,8 @@ __device__ void prefix_of(const AppendArgs& a, int b, int h0, int heads) {
     if (heads == kShort && n1 - n0 <= kShort) {
         const int t = lane / kShort, h = h0 + lane % kShort;
         const bool mine = n0 + t < n1 && h < last;
+        int at = 0;
+        const int id = mine ? page_of(a, b, before + t, at) : -1;
         double c = mine ? a.alpha[(n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
         if (n1 - n0 > 1) {
 #pragma unroll
@@ -146,74 +152,68 @@ __device__ void prefix_of(const AppendArgs& a, int b, int h0, int heads) {
         }
         if (!mine) return;
         c += cached_c(h);
-        int to = 0;
-        const int id = page_of(a, b, before + t, to);
-        if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + to] = (float)c;
+        if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + at] = (float)c;
         return;
     }
     for (int h = h0; h < last; ++h) prefix_long(a, b, h, n0, n1, before, cached_c(h));
 }
 
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const AppendArgs a) {
-    constexpr int LPR = D / 16, RPW = 64 / LPR;
+    constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
     if ((int)blockIdx.x < a.scan_blocks) {
         const long long i = (long long)blockIdx.x * kAppendWaves + (threadIdx.x >> 6);
         const int units = (a.H + a.scan_heads - 1) / a.scan_heads;
         if (i < (long long)a.B * units) prefix_of(a, (int)(i / units), (int)(i % units) * a.scan_heads, a.scan_heads);
         return;
     }
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
-    const long long first = (long long)(blockIdx.x - a.scan_blocks) * kAppendWaves + wv;
-    for (long long item = first; item < a.items; item += (long long)(gridDim.x - a.scan_blocks) * kAppendWaves) {
-        const long long tile = item / a.ranges;
-        const int x0 = (int)(item - tile * a.ranges) * a.heads, x1 = min(x0 + a.heads, a.H + 2 * a.Hkv);
-        const long long n = tile * RPW + lane / LPR;
-        const int b = n < a.rows ? sequence_of(a.start, a.B, (int)n) : -1;
-        if (b < 0) continue;
-        const int before = a.cached[b];
-        const long long p = (long long)before + ((int)n - a.start[b]);
-        int row = 0;
-        const int id = before >= 0 ? page_of(a, b, p, row) : -1;
+    const int all = (a.Q != nullptr ? a.H : 0) + 2 * a.Hkv, keys = all - 2 * a.Hkv, values = all - a.Hkv;  // numbers of the first key, the first value
+    const long long stride = (long long)(gridDim.x - a.scan_blocks) * kAppendWaves;
+    Frequencies freq;
+    if (a.rot > 0) freq.load(l, a.freq);
+    for (long long item = (long long)(blockIdx.x - a.scan_blocks) * kAppendWaves + wv; item < a.shares.items; item += stride) {
+        long long tile;
+        const HeadRange range = a.shares.range(item, tile);
+        const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
+        const long long n = tile * RPW + lane / (LPR * HG), at = min(n, (long long)a.rows - 1);
+        // the row's sequence, position and place in the cache, looked up while its first head is on its way
+        int b = -2, row = 0, id = -1;
+        long long p = 0;
         Angles angles;
-        if (x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, (int)p, a.freq);
-        // rows of `in` to `to`, `step` elements from head to head
-        auto heads_of = [&](const HeadsView& in, const float* weight, T* to, size_t step, int first, int count, bool plain) __attribute__((always_inline)) {
-            const int h0 = max(x0 - first, 0), h1 = min(x1 - first, count);
-            if (h0 >= h1) return;
-            const T* from = (const T*)in.data + n * in.token;
-            LaneWeights w;
-            if (!plain && a.norm) w.load(weight, l);
-            for (int h = h0; h < h1; ++h) {
-                Unit8<T> ua, ub;
-                ua.load(from + h * in.head + l.a);
-                ub.load(from + h * in.head + l.b);
-                if (!plain) {
-                    float x[8], y[8];
-                    ua.get(x);
-                    ub.get(y);
-                    if (a.norm) {
-                        const float r = row_rstd<D>(x, y, a.eps);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[e] *= r * w.a[e];
-                            y[e] *= r * w.b[e];
-                        }
-                    }
-                    if (a.rot > 0) angles.turn<D, false>(l, a.paired, x, y);
-                    ua.set(x);
-                    ub.set(y);
-                }
-                ua.store(to + h * step + l.a);
-                ub.store(to + h * step + l.b);
+        auto look_up = [&]() __attribute__((always_inline)) {
+            if (b != -2) return;
+            int first, before;
+            b = n < a.rows ? sequence_of(a, (int)n, first, before) : -1;
+            if (b >= 0) {
+                p = (long long)before + ((int)n - first);
+                if (before >= 0 && range.x1 > keys) id = page_of(a, b, p, row);
             }
+            if (range.x0 < values && a.rot > 0) angles.at(l, (int)p, freq);
         };
-        if (a.Q != nullptr) heads_of(a.q, a.wq, (T*)a.Q + n * a.H * D, D, 0, a.H, false);
-        if (id < 0) continue;
-        const size_t at = ((size_t)id * a.Hkv * a.page + row) * D, step = (size_t)a.page * D;
-        heads_of(a.k, a.wk, (T*)a.Kp + at, step, a.H, a.Hkv, false);
-        heads_of(a.v, nullptr, (T*)a.Vp + at, step, a.H + a.Hkv, a.Hkv, true);
+        auto heads_of = [&](const HeadsView& in, const float* weight, void* out, int first, int count, auto kind) __attribute__((always_inline)) {
+            constexpr HeadKind K = decltype(kind)::value;
+            int h0, h1;
+            if (!range.part(first, count, h0, h1)) return;
+            const T* const from = (const T*)in.data + at * in.token;
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * in.head, l); };
+            HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
+            LaneVector<D> w;
+            if (K != kValues && a.norm) w.load(weight, l);
+            look_up();
+            const bool there = K == kQueries ? b >= 0 : id >= 0;
+            T* const to = (T*)out + (K == kQueries ? n * a.H * D : ((long long)max(id, 0) * a.Hkv * a.page + row) * D);
+            const size_t step = K == kQueries ? (size_t)D : (size_t)a.page * D;
+            walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                const int h = h0 + i * HG + side;
+                if (K != kValues) r.norm_and_turn(l, a.norm, a.eps, w, a.rot > 0, a.paired, angles);
+                if (there && h < h1) r.template store<ONCE>(to + h * step, l);
+            });
+        };
+        if (a.Q != nullptr) heads_of(a.q, a.wq, a.Q, 0, a.H, std::integral_constant<HeadKind, kQueries>{});
+        heads_of(a.k, a.wk, a.Kp, keys, a.Hkv, std::integral_constant<HeadKind, kKeys>{});
+        heads_of(a.v, nullptr, a.Vp, values, a.Hkv, std::integral_constant<HeadKind, kValues>{});
     }
 }
 
@@ -256,19 +256,19 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.scan_heads = rows > 16LL * B ? 1 : kShort;
     const long long scans = (long long)B * ((H + a.scan_heads - 1) / a.scan_heads);
     a.scan_blocks = alpha != nullptr ? (int)((scans + kAppendWaves - 1) / kAppendWaves) : 0;
-    const int heads = H + 2 * Hkv;
-    const long long tiles = (rows + 1024 / d - 1) / (1024 / d), waves = 16LL * device_cu_count();
-    long long ranges = (waves + tiles - 1) / tiles;
-    if (ranges > heads) ranges = heads;
-    a.heads = (int)((heads + ranges - 1) / ranges);
-    a.ranges = (heads + a.heads - 1) / a.heads;
-    a.items = tiles * a.ranges;
-    long long blocks = (a.items + kAppendWaves - 1) / kAppendWaves;
+    const int side = d == 128 ? kSide<128> : kSide<64>;
+    a.shares = Shares(((long long)rows * side + 1024 / d - 1) / (1024 / d), (Q != nullptr ? H : 0) + 2 * Hkv, side);
+    long long blocks = (a.shares.items + kAppendWaves - 1) / kAppendWaves;
     if (blocks > 1 << 20) blocks = 1 << 20;
     ProfScope prof(kKernAppendPaged, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.scan_blocks + blocks)), dim3(kThreads), 0, s, a); };
-    if (bf16) d == 128 ? launch(append_paged_kernel<bf16_t, 128>) : launch(append_paged_kernel<bf16_t, 64>);
-    else d == 128 ? launch(append_paged_kernel<float, 128>) : launch(append_paged_kernel<float, 64>);
+    if (bf16) {
+        const bool once = rows * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+        if (d == 128) once ? launch(append_paged_kernel<bf16_t, 128, true>) : launch(append_paged_kernel<bf16_t, 128, false>);
+        else launch(append_paged_kernel<bf16_t, 64, false>);
+    } else {
+        d == 128 ? launch(append_paged_kernel<float, 128, false>) : launch(append_paged_kernel<float, 64, false>);
+    }
     return hipGetLastError();
 }
 

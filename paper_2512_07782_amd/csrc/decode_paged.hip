@@ -11,7 +11,6 @@ namespace gfwa {
 namespace {
 
 constexpr int kUnit = 16;       // positions of a unit; pages are multiples of it
-constexpr long long kOnceBytes = 24 << 20;  // windows of more than this are loaded past the caches: the L2s hold 32 MiB
 constexpr float kNone = -1.0e30f;
 
 // Partial result of one (query head, chunk): D output columns (not yet divided by the sum), the exponent they are scaled

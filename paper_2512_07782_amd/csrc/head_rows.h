@@ -2,6 +2,7 @@
 // row, every lane with two units of eight consecutive elements, chosen so that whatever the rotation mixes stands in one lane.
 #pragma once
 #include "gfwa_device.h"
+#include "gfwa_internal.h"
 #include <type_traits>
 
 namespace gfwa {
@@ -12,8 +13,18 @@ struct Unit8;
 template <>
 struct Unit8<bf16_t> {
     bf16x8 v;
-    __device__ __forceinline__ void load(const bf16_t* p) { v = *reinterpret_cast<const bf16x8*>(p); }
-    __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<bf16x8*>(p) = v; }
+    template <bool ONCE = false>
+    __device__ __forceinline__ void load(const bf16_t* p) {
+        const bf16x8* const from = reinterpret_cast<const bf16x8*>(p);
+        if constexpr (ONCE) v = __builtin_nontemporal_load(from);
+        else v = *from;
+    }
+    template <bool PAST = false>
+    __device__ __forceinline__ void store(bf16_t* p) const {
+        bf16x8* const to = reinterpret_cast<bf16x8*>(p);
+        if constexpr (PAST) __builtin_nontemporal_store(v, to);
+        else *to = v;
+    }
     __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
@@ -26,10 +37,12 @@ struct Unit8<bf16_t> {
 template <>
 struct Unit8<float> {
     f32x4 a, b;
+    template <bool ONCE = false>
     __device__ __forceinline__ void load(const float* p) {
         a = reinterpret_cast<const f32x4*>(p)[0];
         b = reinterpret_cast<const f32x4*>(p)[1];
     }
+    template <bool PAST = false>
     __device__ __forceinline__ void store(float* p) const {
         reinterpret_cast<f32x4*>(p)[0] = a;
         reinterpret_cast<f32x4*>(p)[1] = b;
@@ -82,17 +95,33 @@ __device__ __forceinline__ void cos_sin_of(int p, double freq, float& c, float& 
     sincospif((float)t, &s, &c);
 }
 
+// A lane's eight frequencies.
+struct Frequencies {
+    double x[8];
+    template <int D>
+    __device__ __forceinline__ void load(const LaneOfRow<D>& l, const double* freq) {
+        typedef double f64x2 __attribute__((ext_vector_type(2), aligned(8)));
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            f64x2 v = {0.0, 0.0};
+            if (e < 4 ? l.turn_a : l.turn_b) v = *reinterpret_cast<const f64x2*>(freq + (e < 4 ? l.m + e : l.mb + e - 4));
+            x[e] = v[0];
+            x[e + 1] = v[1];
+        }
+    }
+};
+
 // The eight angles of a lane at position p.
 struct Angles {
     float c[8], s[8];
     template <int D>
-    __device__ __forceinline__ void at(const LaneOfRow<D>& l, int p, const double* freq) {
+    __device__ __forceinline__ void at(const LaneOfRow<D>& l, int p, const Frequencies& f) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool turn = e < 4 ? l.turn_a : l.turn_b;
             c[e] = 1.f;
             s[e] = 0.f;
-            if (turn) cos_sin_of(p, freq[e < 4 ? l.m + e : l.mb + e - 4], c[e], s[e]);
+            if (turn) cos_sin_of(p, f.x[e], c[e], s[e]);
         }
     }
     // The two units of a row turned by the angles (BACK: by their negatives).  Elements that are not rotated are left alone, not multiplied by
@@ -144,16 +173,125 @@ __device__ __forceinline__ float row_rstd(const float (&x)[8], const float (&y)[
     return 1.f / sqrtf(mean);
 }
 
-// A lane's sixteen weights of the norm, ones where there are none.
-struct LaneWeights {
+// A lane's sixteen values of a vector of D: weights of the norm, ones where there are none.
+template <int D>
+struct LaneVector {
     float a[8], b[8];
-    template <int D>
     __device__ __forceinline__ void load(const float* w, const LaneOfRow<D>& l) {
+        typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            a[e] = w != nullptr ? w[l.a + e] : 1.f;
-            b[e] = w != nullptr ? w[l.b + e] : 1.f;
+        for (int e = 0; e < 8; e += 4) {
+            f32x4_any x = {1.f, 1.f, 1.f, 1.f}, y = x;
+            if (w != nullptr) {
+                x = *reinterpret_cast<const f32x4_any*>(w + l.a + e);
+                y = *reinterpret_cast<const f32x4_any*>(w + l.b + e);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[e + i] = x[i];
+                b[e + i] = y[i];
+            }
         }
+    }
+};
+
+// The two units of a lane's row.
+// ONCE: loaded past the caches, where a load takes whole lines (bf16, D = 128).  Inputs that the L2s do not hold are read faster (us, H 32, Hkv 8,
+// N 16384: forward 86 -> 74, backward 127 -> 107), those that they may still hold from their making as before.
+template <typename T, int D>
+constexpr bool kWholeLines = sizeof(T) == 2 && D == 128;
+constexpr long long kOnceBytes = 24 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
+template <typename T, int D, bool ONCE = false>
+struct LaneRow {
+    Unit8<T> a, b;
+    __device__ __forceinline__ void load(const T* row, const LaneOfRow<D>& l) {
+        a.template load<ONCE && kWholeLines<T, D>>(row + l.a);
+        b.template load<ONCE && kWholeLines<T, D>>(row + l.b);
+    }
+    // PAST: stored past the caches, for what nothing reads soon.  (Stored like that, the results of norm and rotation cost less themselves, us, H 32,
+    // Hkv 8, N 16384: forward 88 -> 84, backward 129 -> 121, and the kernel that reads them right after more: rope and attention in a row 226
+    // -> 233, at B 4, H 16, Hkv 4, N 4096, d 64 73 -> 78, the backward and a matrix product with its result 407 -> 412.)
+    template <bool PAST = false>
+    __device__ __forceinline__ void store(T* row, const LaneOfRow<D>& l) const {
+        a.template store<PAST>(row + l.a);
+        b.template store<PAST>(row + l.b);
+    }
+    // norm (with weights w) and rotation
+    __device__ __forceinline__ void norm_and_turn(const LaneOfRow<D>& l, bool norm, float eps, const LaneVector<D>& w, bool rotated, bool paired,
+                                                  const Angles& angles) {
+        float x[8], y[8];
+        a.get(x);
+        b.get(y);
+        if (norm) {
+            const float r = row_rstd<D>(x, y, eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] *= r * w.a[e];
+                y[e] *= r * w.b[e];
+            }
+        }
+        if (rotated) angles.template turn<D, false>(l, paired, x, y);
+        a.set(x);
+        b.set(y);
+    }
+};
+
+// Heads of a token that a wave takes side by side: what it reads of a token-major tensor comes in runs of kSide rows, what it writes of a head-major one in
+// runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16384, d 128 89 / 83 / 85 / 88, of N 16640 99 / 96 /
+// 89 / -, backward of N 16640 167 / 147 / 125 / -, append of 16 prompts 119 / 108 / 106 / 125; rows of 4 lanes: backward of B 4, H 16, Hkv 4, N 4096,
+// d 64 39.5 / 35.5 / 39.8 / 51.)
+template <int D>
+constexpr int kSide = D == 128 ? 4 : 2;
+
+// Calls work(row, h) for the heads h0 <= h < h1; the next head's row is on its way meanwhile.  The first
+// one is asked for at once, so that something else can be waited for in between.
+template <typename R, typename Load>
+struct HeadWalk {
+    R row[2];
+    Load load;  // load(row, h)
+    int h0, h1;
+    __device__ __forceinline__ HeadWalk(int from, int to, Load l) : load(l), h0(from), h1(to) { load(row[0], h0); }
+    template <typename Work>
+    __device__ __forceinline__ void run(Work&& work) {
+        for (int h = h0; h < h1; h += 2) {
+            if (h + 1 < h1) load(row[1], h + 1);
+            work(row[0], h);
+            if (h + 1 >= h1) break;
+            if (h + 2 < h1) load(row[0], h + 2);
+            work(row[1], h + 1);
+        }
+    }
+};
+
+// The heads of a token in one row of numbers: queries, then keys, then values.  A wave takes a range of them.
+enum HeadKind { kQueries = 0, kKeys = 1, kValues = 2 };
+struct HeadRange {
+    int x0, x1;
+    // the heads h0 <= h < h1 of a kind whose `count` heads begin at number `first`
+    __device__ __forceinline__ bool part(int first, int count, int& h0, int& h1) const {
+        h0 = max(x0 - first, 0);
+        h1 = min(x1 - first, count);
+        return h0 < h1;
+    }
+};
+// How `tiles` tiles of tokens and `heads` heads are shared out over the waves: ranges of heads as long as still leave every SIMD two waves
+// (what a wave finds out about a token serves all heads of its range).
+struct Shares {
+    int ranges, heads;  // ranges, and heads of one
+    long long items;    // tiles x ranges
+    Shares() = default;
+    Shares(long long tiles, int all, int side) {  // ranges are multiples of `side` heads
+        long long want = (8LL * device_cu_count() + tiles - 1) / tiles;
+        if (want > all) want = all;
+        heads = (int)((all + want - 1) / want);
+        heads = (heads + side - 1) / side * side;
+        ranges = (all + heads - 1) / heads;
+        items = tiles * ranges;
+    }
+    __device__ __forceinline__ HeadRange range(long long item, long long& tile) const {
+        tile = item >> 31 == 0 ? (unsigned)item / (unsigned)ranges : item / ranges;
+        const int x0 = (int)(item - tile * ranges) * heads;
+        return {x0, x0 + heads};
     }
 };
 

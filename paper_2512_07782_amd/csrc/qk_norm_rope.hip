@@ -3,8 +3,8 @@
 // the attention's head-major layout (or back).
 //   * a row of D elements is held by D / 16 lanes (head_rows.h), so that the norm's sum takes two or three DPP exchanges, the rotation
 //     none, and every access is whole 16-byte pieces;
-//   * a wave takes 1024 / D consecutive tokens and walks over a range of heads: a token's angles are formed once for all of them, and
-//     what it writes for a head is one run of 2048 elements or less of the head-major layout;
+//   * a wave takes two (D = 128) or eight (D = 64) consecutive tokens, four or two heads of each at a time, and walks over a range of heads: a token's
+//     angles are formed once for all of them, and both layouts are met in runs (kSide);
 //   * the weights' gradients are summed in registers over all rows of a wave, over the waves through LDS and over the workgroups by
 //     a second small launch, in an order that does not change from run to run.
 #include "gfwa_internal.h"
@@ -29,8 +29,7 @@ struct RopeArgs {
     float* part;           // backward: the workgroups' sums of the weights' gradients, [workgroups][2][D], or nullptr
     int H, Hkv, N;
     long long tokens;      // B * N
-    long long items;       // token tiles x head ranges
-    int ranges, heads;     // head ranges and heads of one
+    Shares shares;         // of tiles of 1024 / D tokens
 };
 
 // A lane's token: where its rows stand in the token-major and the head-major layout.
@@ -40,198 +39,200 @@ struct LaneToken {
     __device__ __forceinline__ LaneToken(long long t, const RopeArgs& a) {
         there = t < a.tokens;
         flat = there ? t : a.tokens - 1;
-        b = flat / a.N;
+        if (flat >> 31 == 0) {  // 64-bit quotients take several times as long
+            b = (unsigned)flat / (unsigned)a.N;
+        } else {
+            b = flat / a.N;
+        }
         n = flat - b * a.N;
     }
 };
 
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const RopeArgs a) {
-    constexpr int LPR = D / 16, RPW = 64 / LPR;
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
-    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.items; item += (long long)gridDim.x * kRopeWaves) {
-        const long long tile = item / a.ranges;
-        const int x0 = (int)(item - tile * a.ranges) * a.heads, x1 = min(x0 + a.heads, a.H + 2 * a.Hkv);
-        const LaneToken t(tile * RPW + lane / LPR, a);
+    Frequencies freq;
+    if (a.rot > 0) freq.load(l, a.freq);
+    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += (long long)gridDim.x * kRopeWaves) {
+        long long tile;
+        const HeadRange range = a.shares.range(item, tile);
+        const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
+        const LaneToken t(tile * RPW + lane / (LPR * HG), a);
         Angles angles;
-        if (x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, a.freq);
-        auto heads_of = [&](const HeadsView& in, const float* weight, void* out, int first, int count, bool plain) __attribute__((always_inline)) {
-            const int h0 = max(x0 - first, 0), h1 = min(x1 - first, count);
-            if (h0 >= h1) return;
-            const T* from = (const T*)in.data + t.b * in.batch + t.n * in.token;
-            T* to = (T*)out + (t.b * count * a.N + t.n) * D;
-            LaneWeights w;
-            if (!plain && a.norm) w.load(weight, l);
-            for (int h = h0; h < h1; ++h) {
-                Unit8<T> ua, ub;
-                ua.load(from + h * in.head + l.a);
-                ub.load(from + h * in.head + l.b);
-                if (!plain) {
-                    float x[8], y[8];
-                    ua.get(x);
-                    ub.get(y);
-                    if (a.norm) {
-                        const float r = row_rstd<D>(x, y, a.eps);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[e] *= r * w.a[e];
-                            y[e] *= r * w.b[e];
-                        }
-                    }
-                    if (a.rot > 0) angles.turn<D, false>(l, a.paired, x, y);
-                    ua.set(x);
-                    ub.set(y);
-                }
-                if (t.there) {
-                    ua.store(to + (size_t)h * a.N * D + l.a);
-                    ub.store(to + (size_t)h * a.N * D + l.b);
-                }
-            }
-        };
-        heads_of(a.q, a.wq, a.Q, 0, a.H, false);
-        heads_of(a.k, a.wk, a.K, a.H, a.Hkv, false);
-        if (a.V != nullptr) heads_of(a.v, nullptr, a.V, a.H + a.Hkv, a.Hkv, true);
+        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, freq);
+#pragma unroll 1
+        for (int kind = kQueries; kind <= kKeys; ++kind) {
+            const bool keys = kind == kKeys;
+            const int count = keys ? a.Hkv : a.H;
+            int h0, h1;
+            if (!range.part(keys ? a.H : 0, count, h0, h1)) continue;
+            const HeadsView in = keys ? a.k : a.q;
+            const T* const from = (const T*)in.data + t.b * in.batch + t.n * in.token;
+            T* const to = (T*)(keys ? a.K : a.Q) + (t.b * count * a.N + t.n) * D;
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * in.head, l); };
+            HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
+            LaneVector<D> w;
+            if (a.norm) w.load(keys ? a.wk : a.wq, l);
+            walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                const int h = h0 + i * HG + side;
+                r.norm_and_turn(l, a.norm, a.eps, w, a.rot > 0, a.paired, angles);
+                if (t.there && h < h1) r.store(to + (size_t)h * a.N * D, l);
+            });
+        }
+        int h0, h1;
+        if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
+            const T* const from = (const T*)a.v.data + t.b * a.v.batch + t.n * a.v.token;
+            T* const to = (T*)a.V + (t.b * a.Hkv * a.N + t.n) * D;
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * a.v.head, l); };
+            HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
+            walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                const int h = h0 + i * HG + side;
+                if (t.there && h < h1) r.store(to + (size_t)h * a.N * D, l);
+            });
+        }
     }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const RopeArgs a) {
-    constexpr int LPR = D / 16, RPW = 64 / LPR;
-    __shared__ float sums[kRopeWaves][2][D];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
+    __shared__ float sums[kRopeWaves][2][16][64];  // of each lane's elements, for the queries' and the keys' weights
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
-    LaneWeights dwq, dwk;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dwq.a[e] = dwq.b[e] = dwk.a[e] = dwk.b[e] = 0.f;
-    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.items; item += (long long)gridDim.x * kRopeWaves) {
-        const long long tile = item / a.ranges;
-        const int x0 = (int)(item - tile * a.ranges) * a.heads, x1 = min(x0 + a.heads, a.H + 2 * a.Hkv);
-        const LaneToken t(tile * RPW + lane / LPR, a);
+    for (int i = 0; i < 32; ++i) sums[wv][i >> 4][i & 15][lane] = 0.f;
+    struct Rows {
+        LaneRow<T, D, ONCE> g, x;
+    };
+    Frequencies freq;
+    if (a.rot > 0) freq.load(l, a.freq);
+    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += (long long)gridDim.x * kRopeWaves) {
+        long long tile;
+        const HeadRange range = a.shares.range(item, tile);
+        const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
+        const LaneToken t(tile * RPW + lane / (LPR * HG), a);
         Angles angles;
-        if (x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, a.freq);
-        auto heads_of = [&](const HeadsView& out, const HeadsView& in, const float* weight, const void* dy, LaneWeights& dw, int first, int count,
-                            bool plain) __attribute__((always_inline)) {
-            const int h0 = max(x0 - first, 0), h1 = min(x1 - first, count);
-            if (h0 >= h1) return;
-            const T* from = (const T*)dy + (t.b * count * a.N + t.n) * D;
-            T* to = (T*)out.data + t.b * out.batch + t.n * out.token;
-            const bool normed = !plain && a.norm;
-            const T* xs = normed ? (const T*)in.data + t.b * in.batch + t.n * in.token : nullptr;
-            LaneWeights w;
-            if (normed) w.load(weight, l);
-            for (int h = h0; h < h1; ++h) {
-                Unit8<T> ga, gb, xa, xb;
-                ga.load(from + (size_t)h * a.N * D + l.a);
-                gb.load(from + (size_t)h * a.N * D + l.b);
-                if (normed) {
-                    xa.load(xs + h * in.head + l.a);
-                    xb.load(xs + h * in.head + l.b);
-                }
-                if (!plain) {
-                    float g[8], f[8];
-                    ga.get(g);
-                    gb.get(f);
-                    if (a.rot > 0) angles.turn<D, true>(l, a.paired, g, f);
-                    if (normed) {
-                        float x[8], y[8];
-                        xa.get(x);
-                        xb.get(y);
-                        const float r = row_rstd<D>(x, y, a.eps);
-                        float dot = 0.f;
+        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, freq);
+#pragma unroll 1
+        for (int kind = kQueries; kind <= kKeys; ++kind) {
+            const bool keys = kind == kKeys;
+            const int count = keys ? a.Hkv : a.H;
+            int h0, h1;
+            if (!range.part(keys ? a.H : 0, count, h0, h1)) continue;
+            const HeadsView out = keys ? a.k : a.q, in = keys ? a.x_k : a.x_q;
+            const T* const from = (const T*)(keys ? a.K : a.Q) + (t.b * count * a.N + t.n) * D;
+            T* const to = (T*)out.data + t.b * out.batch + t.n * out.token;
+            const T* const xs = a.norm ? (const T*)in.data + t.b * in.batch + t.n * in.token : nullptr;
+            auto load = [&](Rows& r, int i) __attribute__((always_inline)) {
+                const int h = min(h0 + i * HG + side, h1 - 1);
+                r.g.load(from + (size_t)h * a.N * D, l);
+                if (a.norm) r.x.load(xs + h * in.head, l);
+            };
+            HeadWalk<Rows, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
+            LaneVector<D> w, dw;
+            if (a.norm) w.load(keys ? a.wk : a.wq, l);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[e] *= r;
-                            y[e] *= r;
-                            dw.a[e] += t.there ? g[e] * x[e] : 0.f;
-                            dw.b[e] += t.there ? f[e] * y[e] : 0.f;
-                            g[e] *= w.a[e];
-                            f[e] *= w.b[e];
-                            dot = fmaf(g[e], x[e], fmaf(f[e], y[e], dot));
-                        }
-                        dot = sum_over_row<LPR>(dot) * (1.f / D);
+            for (int e = 0; e < 8; ++e) dw.a[e] = dw.b[e] = 0.f;
+            walk.run([&](Rows& r, int i) __attribute__((always_inline)) {
+                const int h = h0 + i * HG + side;
+                const bool there = t.there && h < h1;
+                float g[8], f[8];
+                r.g.a.get(g);
+                r.g.b.get(f);
+                if (a.rot > 0) angles.turn<D, true>(l, a.paired, g, f);
+                if (a.norm) {
+                    float x[8], y[8];
+                    r.x.a.get(x);
+                    r.x.b.get(y);
+                    const float rstd = row_rstd<D>(x, y, a.eps);
+                    float dot = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            g[e] = r * fmaf(-dot, x[e], g[e]);
-                            f[e] = r * fmaf(-dot, y[e], f[e]);
-                        }
+                    for (int e = 0; e < 8; ++e) {
+                        x[e] *= rstd;
+                        y[e] *= rstd;
+                        dw.a[e] = fmaf(there ? g[e] : 0.f, x[e], dw.a[e]);
+                        dw.b[e] = fmaf(there ? f[e] : 0.f, y[e], dw.b[e]);
+                        g[e] *= w.a[e];
+                        f[e] *= w.b[e];
+                        dot = fmaf(g[e], x[e], fmaf(f[e], y[e], dot));
                     }
-                    ga.set(g);
-                    gb.set(f);
-                }
-                if (t.there) {
-                    ga.store(to + h * out.head + l.a);
-                    gb.store(to + h * out.head + l.b);
-                }
-            }
-        };
-        heads_of(a.q, a.x_q, a.wq, a.Q, dwq, 0, a.H, false);
-        heads_of(a.k, a.x_k, a.wk, a.K, dwk, a.H, a.Hkv, false);
-        if (a.V != nullptr) heads_of(a.v, a.x_k, nullptr, a.V, dwk, a.H + a.Hkv, a.Hkv, true);
-    }
-    if (a.part == nullptr) return;  // uniform over the launch
-    // over the tokens of the wave, then over the waves
-    auto over_tokens = [&](LaneWeights& dw, int which) __attribute__((always_inline)) {
+                    dot = sum_over_row<LPR>(dot) * (1.f / D);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+                    for (int e = 0; e < 8; ++e) {
+                        g[e] = rstd * fmaf(-dot, x[e], g[e]);
+                        f[e] = rstd * fmaf(-dot, y[e], f[e]);
+                    }
+                }
+                r.g.a.set(g);
+                r.g.b.set(f);
+                if (there) r.g.store(to + h * out.head, l);
+            });
+            if (a.part != nullptr) {  // the lane's own cells
 #pragma unroll
-            for (int off = LPR; off < 64; off <<= 1) {
-                dw.a[e] += __shfl_xor(dw.a[e], off, 64);
-                dw.b[e] += __shfl_xor(dw.b[e], off, 64);
-            }
-            if (lane < LPR) {
-                sums[wv][which][l.a + e] = dw.a[e];
-                sums[wv][which][l.b + e] = dw.b[e];
+                for (int e = 0; e < 8; ++e) {
+                    sums[wv][kind][e][lane] += dw.a[e];
+                    sums[wv][kind][8 + e][lane] += dw.b[e];
+                }
             }
         }
-    };
-    over_tokens(dwq, 0);
-    over_tokens(dwk, 1);
+        int h0, h1;
+        if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
+            const T* const from = (const T*)a.V + (t.b * a.Hkv * a.N + t.n) * D;
+            T* const to = (T*)a.v.data + t.b * a.v.batch + t.n * a.v.token;
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + (size_t)min(h0 + i * HG + side, h1 - 1) * a.N * D, l); };
+            HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
+            walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                const int h = h0 + i * HG + side;
+                if (t.there && h < h1) r.store(to + h * a.v.head, l);
+            });
+        }
+    }
+    if (a.part == nullptr) return;  // uniform over the launch
     __syncthreads();
+    // over the tokens of a wave (lanes j, j + LPR, ..) and over the waves
     for (int i = threadIdx.x; i < 2 * D; i += 64 * kRopeWaves) {
+        const int kind = i / D, j = i % LPR, e = i % D / LPR;  // element e of lane j
         float s = 0.f;
+        for (int k = 0; k < kRopeWaves; ++k)
 #pragma unroll
-        for (int k = 0; k < kRopeWaves; ++k) s += sums[k][i / D][i % D];
-        a.part[(size_t)blockIdx.x * 2 * D + i] = s;
+            for (int row = 0; row < 64 / LPR; ++row) s += sums[k][kind][e][row * LPR + j];
+        const LaneOfRow<D> of(j, a.rot, a.paired);
+        a.part[(size_t)blockIdx.x * 2 * D + kind * D + (e < 8 ? of.a + e : of.b + e - 8)] = s;
     }
 }
 
-// dw[i] = sum over the workgroups of part[., i]: one workgroup for 32 sums, 32 partial rows at a time.
+// dw[i] = sum over the workgroups of part[., i]: one workgroup for 16 of the 2 D sums, 64 partial rows at a time.
 __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __restrict__ part, float* dwq, float* dwk, int blocks, int D) {
-    __shared__ float sums[32][33];
-    const int col = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int i = blockIdx.x * 32 + col;  // 2 D is a multiple of 32
+    __shared__ float sums[64][17];
+    const int col = threadIdx.x & 15, row = threadIdx.x >> 4;
+    const int i = blockIdx.x * 16 + col;
+    float* const dw = i < D ? dwq : dwk;
     float s = 0.f;
-    for (int k = row; k < blocks; k += 32) s += part[(size_t)k * 2 * D + i];
+#pragma unroll 8
+    for (int k = row; k < blocks; k += 64) s += part[(size_t)k * 2 * D + i];
     sums[row][col] = s;
     __syncthreads();
-    if (row == 0) {
+    if (row == 0 && dw != nullptr) {
         s = 0.f;
-        for (int k = 0; k < 32; ++k) s += sums[k][col];
-        float* dw = i < D ? dwq : dwk;
-        if (dw != nullptr) dw[i % D] = s;
+        for (int k = 0; k < 64; ++k) s += sums[k][col];
+        dw[i % D] = s;
     }
 }
 
-// How the work is cut up: head ranges as long as still leave every SIMD its waves.
-void cut(RopeArgs& a, int D, long long& blocks, long long most_blocks) {
-    const int heads = a.H + (a.V != nullptr ? 2 : 1) * a.Hkv;
-    const long long tiles = (a.tokens + 1024 / D - 1) / (1024 / D);
-    const long long waves = 16LL * device_cu_count();
-    long long ranges = (waves + tiles - 1) / tiles;
-    if (ranges > heads) ranges = heads;
-    a.heads = (int)((heads + ranges - 1) / ranges);
-    a.ranges = (heads + a.heads - 1) / a.heads;
-    a.items = tiles * a.ranges;
-    blocks = (a.items + kRopeWaves - 1) / kRopeWaves;
-    if (blocks > most_blocks) blocks = most_blocks;
-}
+constexpr int kMostSums = 2048;  // workgroups that leave sums of the weights' gradients
 
-long long most_bwd_blocks() { return 8LL * 256; }
+long long share_out(RopeArgs& a, int D, long long most) {
+    const int side = D == 128 ? kSide<128> : kSide<64>;
+    a.shares = Shares((a.tokens * side + 1024 / D - 1) / (1024 / D), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
+    const long long blocks = (a.shares.items + kRopeWaves - 1) / kRopeWaves;
+    return blocks < most ? blocks : most;
+}
 
 }  // namespace
 
-size_t qk_norm_rope_backward_workspace_bytes(int d) { return (size_t)most_bwd_blocks() * 2 * d * sizeof(float); }
+size_t qk_norm_rope_backward_workspace_bytes(int d) { return (size_t)kMostSums * 2 * d * sizeof(float); }
 
 static RopeArgs rope_args(const HeadRotation& how, void* Q, void* K, void* V, int B, int H, int Hkv, int N) {
     RopeArgs a{};
@@ -259,12 +260,16 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.q = q;
     a.k = k;
     a.v = v;
-    long long blocks;
-    cut(a, d, blocks, 1 << 20);
+    const long long blocks = share_out(a, d, 1 << 20);
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
-    if (bf16) d == 128 ? launch(qk_norm_rope_kernel<bf16_t, 128>) : launch(qk_norm_rope_kernel<bf16_t, 64>);
-    else d == 128 ? launch(qk_norm_rope_kernel<float, 128>) : launch(qk_norm_rope_kernel<float, 64>);
+    if (bf16) {
+        const bool once = a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+        if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_kernel<bf16_t, 128, false>);
+        else launch(qk_norm_rope_kernel<bf16_t, 64, false>);
+    } else {
+        d == 128 ? launch(qk_norm_rope_kernel<float, 128, false>) : launch(qk_norm_rope_kernel<float, 64, false>);
+    }
     return hipGetLastError();
 }
 
@@ -278,17 +283,21 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.x_q = q;
     a.x_k = k;
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
-    long long blocks;
-    cut(a, d, blocks, most_bwd_blocks());
+    const long long blocks = share_out(a, d, a.part != nullptr ? kMostSums : 1 << 20);
     {
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
-        if (bf16) d == 128 ? launch(qk_norm_rope_bwd_kernel<bf16_t, 128>) : launch(qk_norm_rope_bwd_kernel<bf16_t, 64>);
-        else d == 128 ? launch(qk_norm_rope_bwd_kernel<float, 128>) : launch(qk_norm_rope_bwd_kernel<float, 64>);
+        if (bf16) {
+            const bool once = a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+            if (d == 128) once ? launch(qk_norm_rope_bwd_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_bwd_kernel<bf16_t, 128, false>);
+            else launch(qk_norm_rope_bwd_kernel<bf16_t, 64, false>);
+        } else {
+            d == 128 ? launch(qk_norm_rope_bwd_kernel<float, 128, false>) : launch(qk_norm_rope_bwd_kernel<float, 64, false>);
+        }
     }
     if (a.part != nullptr) {
         ProfScope prof(kKernNormWeightSum, s);
-        hipLaunchKernelGGL(weight_grad_sum_kernel, dim3(2 * d / 32), dim3(1024), 0, s, part, dwq, dwk, (int)blocks, d);
+        hipLaunchKernelGGL(weight_grad_sum_kernel, dim3(2 * d / 16), dim3(1024), 0, s, part, dwq, dwk, (int)blocks, d);
     }
     return hipGetLastError();
 }
