@@ -170,14 +170,13 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const A
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
     const int all = (a.Q != nullptr ? a.H : 0) + 2 * a.Hkv, keys = all - 2 * a.Hkv, values = all - a.Hkv;  // numbers of the first key, the first value
-    const long long stride = (long long)(gridDim.x - a.scan_blocks) * kAppendWaves;
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
-    for (long long item = (long long)(blockIdx.x - a.scan_blocks) * kAppendWaves + wv; item < a.shares.items; item += stride) {
-        long long tile;
+    for (int item = (blockIdx.x - a.scan_blocks) * kAppendWaves + wv; item < a.shares.items; item += (gridDim.x - a.scan_blocks) * kAppendWaves) {
+        int tile;
         const HeadRange range = a.shares.range(item, tile);
         const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
-        const long long n = tile * RPW + lane / (LPR * HG), at = min(n, (long long)a.rows - 1);
+        const long long n = (long long)tile * RPW + lane / (LPR * HG), at = min(n, (long long)a.rows - 1);
         // the row's sequence, position and place in the cache, looked up while its first head is on its way
         int b = -2, row = 0, id = -1;
         long long p = 0;
@@ -257,8 +256,8 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     const long long scans = (long long)B * ((H + a.scan_heads - 1) / a.scan_heads);
     a.scan_blocks = alpha != nullptr ? (int)((scans + kAppendWaves - 1) / kAppendWaves) : 0;
     const int side = d == 128 ? kSide<128> : kSide<64>;
-    a.shares = Shares(((long long)rows * side + 1024 / d - 1) / (1024 / d), (Q != nullptr ? H : 0) + 2 * Hkv, side);
-    long long blocks = (a.shares.items + kAppendWaves - 1) / kAppendWaves;
+    a.shares = Shares((int)(((long long)rows * side + 1024 / d - 1) / (1024 / d)), (Q != nullptr ? H : 0) + 2 * Hkv, side);
+    long long blocks = ((long long)a.shares.items + kAppendWaves - 1) / kAppendWaves;
     if (blocks > 1 << 20) blocks = 1 << 20;
     ProfScope prof(kKernAppendPaged, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.scan_blocks + blocks)), dim3(kThreads), 0, s, a); };

@@ -278,19 +278,19 @@ struct HeadRange {
 // (what a wave finds out about a token serves all heads of its range).
 struct Shares {
     int ranges, heads;  // ranges, and heads of one
-    long long items;    // tiles x ranges
+    int items;          // tiles x ranges: more than one range only where there are few tiles
     Shares() = default;
-    Shares(long long tiles, int all, int side) {  // ranges are multiples of `side` heads
-        long long want = (8LL * device_cu_count() + tiles - 1) / tiles;
+    Shares(int tiles, int all, int side) {  // ranges are multiples of `side` heads
+        int want = tiles < 8 * device_cu_count() ? (8 * device_cu_count() + tiles - 1) / tiles : 1;
         if (want > all) want = all;
-        heads = (int)((all + want - 1) / want);
+        heads = (all + want - 1) / want;
         heads = (heads + side - 1) / side * side;
         ranges = (all + heads - 1) / heads;
         items = tiles * ranges;
     }
-    __device__ __forceinline__ HeadRange range(long long item, long long& tile) const {
-        tile = item >> 31 == 0 ? (unsigned)item / (unsigned)ranges : item / ranges;
-        const int x0 = (int)(item - tile * ranges) * heads;
+    __device__ __forceinline__ HeadRange range(int item, int& tile) const {
+        tile = item / ranges;
+        const int x0 = (item - tile * ranges) * heads;
         return {x0, x0 + heads};
     }
 };

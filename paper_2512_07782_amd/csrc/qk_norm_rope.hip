@@ -28,24 +28,22 @@ struct RopeArgs {
     void *Q, *K, *V;       // head-major, dense (backward: dQ, dK, dV are read)
     float* part;           // backward: the workgroups' sums of the weights' gradients, [workgroups][2][D], or nullptr
     int H, Hkv, N;
-    long long tokens;      // B * N
+    int tokens;            // B * N
     Shares shares;         // of tiles of 1024 / D tokens
 };
 
 // A lane's token: where its rows stand in the token-major and the head-major layout.
 struct LaneToken {
     bool there;
-    long long b, n, flat;
+    int b, n, flat;
     __device__ __forceinline__ LaneToken(long long t, const RopeArgs& a) {
         there = t < a.tokens;
-        flat = there ? t : a.tokens - 1;
-        if (flat >> 31 == 0) {  // 64-bit quotients take several times as long
-            b = (unsigned)flat / (unsigned)a.N;
-        } else {
-            b = flat / a.N;
-        }
+        flat = there ? (int)t : a.tokens - 1;
+        b = flat / a.N;
         n = flat - b * a.N;
     }
+    __device__ __forceinline__ long long in(const HeadsView& x) const { return b * x.batch + n * x.token; }
+    __device__ __forceinline__ long long dense(int heads, int N) const { return (long long)b * heads * N + n; }  // row of the first head
 };
 
 template <typename T, int D, bool ONCE>
@@ -55,13 +53,13 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
-    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += (long long)gridDim.x * kRopeWaves) {
-        long long tile;
+    for (int item = blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += gridDim.x * kRopeWaves) {
+        int tile;
         const HeadRange range = a.shares.range(item, tile);
         const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
-        const LaneToken t(tile * RPW + lane / (LPR * HG), a);
+        const LaneToken t((long long)tile * RPW + lane / (LPR * HG), a);
         Angles angles;
-        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, freq);
+        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : t.n, freq);
 #pragma unroll 1
         for (int kind = kQueries; kind <= kKeys; ++kind) {
             const bool keys = kind == kKeys;
@@ -69,8 +67,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
             int h0, h1;
             if (!range.part(keys ? a.H : 0, count, h0, h1)) continue;
             const HeadsView in = keys ? a.k : a.q;
-            const T* const from = (const T*)in.data + t.b * in.batch + t.n * in.token;
-            T* const to = (T*)(keys ? a.K : a.Q) + (t.b * count * a.N + t.n) * D;
+            const T* const from = (const T*)in.data + t.in(in);
+            T* const to = (T*)(keys ? a.K : a.Q) + t.dense(count, a.N) * D;
             auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * in.head, l); };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             LaneVector<D> w;
@@ -83,8 +81,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
         }
         int h0, h1;
         if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
-            const T* const from = (const T*)a.v.data + t.b * a.v.batch + t.n * a.v.token;
-            T* const to = (T*)a.V + (t.b * a.Hkv * a.N + t.n) * D;
+            const T* const from = (const T*)a.v.data + t.in(a.v);
+            T* const to = (T*)a.V + t.dense(a.Hkv, a.N) * D;
             auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * a.v.head, l); };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
@@ -108,13 +106,13 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
     };
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
-    for (long long item = (long long)blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += (long long)gridDim.x * kRopeWaves) {
-        long long tile;
+    for (int item = blockIdx.x * kRopeWaves + wv; item < a.shares.items; item += gridDim.x * kRopeWaves) {
+        int tile;
         const HeadRange range = a.shares.range(item, tile);
         const int side = lane / LPR % HG;  // this lane's head of the HG next to each other
-        const LaneToken t(tile * RPW + lane / (LPR * HG), a);
+        const LaneToken t((long long)tile * RPW + lane / (LPR * HG), a);
         Angles angles;
-        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : (int)t.n, freq);
+        if (range.x0 < a.H + a.Hkv && a.rot > 0) angles.at(l, a.pos != nullptr ? a.pos[t.flat] : t.n, freq);
 #pragma unroll 1
         for (int kind = kQueries; kind <= kKeys; ++kind) {
             const bool keys = kind == kKeys;
@@ -122,9 +120,9 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
             int h0, h1;
             if (!range.part(keys ? a.H : 0, count, h0, h1)) continue;
             const HeadsView out = keys ? a.k : a.q, in = keys ? a.x_k : a.x_q;
-            const T* const from = (const T*)(keys ? a.K : a.Q) + (t.b * count * a.N + t.n) * D;
-            T* const to = (T*)out.data + t.b * out.batch + t.n * out.token;
-            const T* const xs = a.norm ? (const T*)in.data + t.b * in.batch + t.n * in.token : nullptr;
+            const T* const from = (const T*)(keys ? a.K : a.Q) + t.dense(count, a.N) * D;
+            T* const to = (T*)out.data + t.in(out);
+            const T* const xs = a.norm ? (const T*)in.data + t.in(in) : nullptr;
             auto load = [&](Rows& r, int i) __attribute__((always_inline)) {
                 const int h = min(h0 + i * HG + side, h1 - 1);
                 r.g.load(from + (size_t)h * a.N * D, l);
@@ -179,8 +177,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
         }
         int h0, h1;
         if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
-            const T* const from = (const T*)a.V + (t.b * a.Hkv * a.N + t.n) * D;
-            T* const to = (T*)a.v.data + t.b * a.v.batch + t.n * a.v.token;
+            const T* const from = (const T*)a.V + t.dense(a.Hkv, a.N) * D;
+            T* const to = (T*)a.v.data + t.in(a.v);
             auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + (size_t)min(h0 + i * HG + side, h1 - 1) * a.N * D, l); };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
@@ -225,8 +223,8 @@ constexpr int kMostSums = 2048;  // workgroups that leave sums of the weights' g
 
 long long share_out(RopeArgs& a, int D, long long most) {
     const int side = D == 128 ? kSide<128> : kSide<64>;
-    a.shares = Shares((a.tokens * side + 1024 / D - 1) / (1024 / D), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
-    const long long blocks = (a.shares.items + kRopeWaves - 1) / kRopeWaves;
+    a.shares = Shares((int)(((long long)a.tokens * side + 1024 / D - 1) / (1024 / D)), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
+    const long long blocks = ((long long)a.shares.items + kRopeWaves - 1) / kRopeWaves;
     return blocks < most ? blocks : most;
 }
 
@@ -250,7 +248,7 @@ static RopeArgs rope_args(const HeadRotation& how, void* Q, void* K, void* V, in
     a.H = H;
     a.Hkv = Hkv;
     a.N = N;
-    a.tokens = (long long)B * N;
+    a.tokens = B * N;
     return a;
 }
 
@@ -264,7 +262,7 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
     if (bf16) {
-        const bool once = a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+        const bool once = (long long)a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
         if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_kernel<bf16_t, 128, false>);
         else launch(qk_norm_rope_kernel<bf16_t, 64, false>);
     } else {
@@ -288,7 +286,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
         if (bf16) {
-            const bool once = a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+            const bool once = (long long)a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
             if (d == 128) once ? launch(qk_norm_rope_bwd_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_bwd_kernel<bf16_t, 128, false>);
             else launch(qk_norm_rope_bwd_kernel<bf16_t, 64, false>);
         } else {
