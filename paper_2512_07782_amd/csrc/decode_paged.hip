@@ -216,6 +216,9 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // A workgroup takes one chunk of the window for up to 16 query heads of one key/value head, each wave every NW-th tile of it, newest first; loads of
 // the next tile are on their way while a tile is worked on.  A head's weights are taken against a reference that is raised, and sums rescaled,
 // only when a score exceeds it by 2^16.
+// (The page numbers of the tile after that could be asked for ahead too: eight more registers, which bf16 at d = 128 does not have beside three waves a
+// SIMD; whole sequences, H 32, Hkv 8, 4 of up to 8192 22.3 us with and 19.5 without, 16
+// 68.3 and 65.4, 128 windows of 512 keys 49.3 and 51.7.  Two tiles ahead: 22.1, 68.1 and 47.6, in fp32 past the registers.)
 // ONCE: V is loaded past the caches.  No other workgroup reads it, and a window that the L2s do not hold is read faster (us, bf16, H 32, Hkv 8, d 128,
 // w 1024: 64 sequences 49.4 -> 46.0, 32 26.1 -> 22.8; H 32, Hkv 4, d 64, whole sequences of up to 16384 40.7 -> 33.8), one that they do hold more
 // slowly (2 sequences of H 16, d 64, w 512, 4 MB, 6.7 -> 7.2).  K's lines are asked for by two loads each: past the caches 47.6 for the first.
@@ -271,23 +274,19 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
         Tl tile;
         f32x4_any cf[NU];
         bool there[NU];
-        Unit next[NU];
-        auto look_up = [&](int t) __attribute__((always_inline)) {
+        auto issue = [&](int t) __attribute__((always_inline)) {
+            Unit x[NU];
 #pragma unroll
-            for (int n = 0; n < NU; ++n) next[n] = unit(u_hi - NU * t - n);
-        };
-        auto issue = [&]() __attribute__((always_inline)) {
+            for (int n = 0; n < NU; ++n) x[n] = unit(u_hi - NU * t - n);
 #pragma unroll
             for (int n = 0; n < NU; ++n) {
-                there[n] = next[n].there;
-                const size_t at = ((size_t)next[n].page * a.Hkv * a.page + next[n].row) * D;
+                there[n] = x[n].there;
+                const size_t at = ((size_t)x[n].page * a.Hkv * a.page + x[n].row) * D;
                 tile.template load<ONCE>(n, K + at, V + at, lane);
-                cf[n] = *reinterpret_cast<const f32x4_any*>(C + (size_t)next[n].page * a.H * a.page + next[n].row + 4 * g);
+                cf[n] = *reinterpret_cast<const f32x4_any*>(C + (size_t)x[n].page * a.H * a.page + x[n].row + 4 * g);
             }
         };
-        look_up(t);
-        issue();
-        if (t + NW < t1) look_up(t + NW);
+        issue(t);
         for (; t < t1; t += NW) {
             const int key0 = (u_hi - NU * t) * kUnit;  // first key of the newest unit
             bool whole = key0 - (NU - 1) * kUnit >= me.lo && key0 + kUnit - 1 <= me.p, was[NU];
@@ -312,10 +311,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
             for (int n = 0; n < NU; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) bias[n][e] = (cf[n][e] - c0) * kLog2e;
-            if (t + NW < t1) {
-                issue();
-                if (t + 2 * NW < t1) look_up(t + 2 * NW);
-            }
+            if (t + NW < t1) issue(t + NW);
             __builtin_amdgcn_sched_barrier(0);
             float top = -INFINITY;
 #pragma unroll
