@@ -193,6 +193,60 @@ def decode_only(args, g, torch) -> int:
     return 0
 
 
+def decode_paged_only(args, g, torch) -> int:
+    """A serving step against the paged cache: the new tokens' norm, rotation and append, then the decoding step, HBM-bound on reading the
+    window once.  Every sequence at position T-1, its pages shuffled; with a window only the pages it touches exist."""
+    B, H, Hkv, T, d, w = (int(x) for x in args.decode.split(","))
+    page, dev, n = args.paged, "cuda:0", min(w, T)
+    gen = torch.Generator(device=dev).manual_seed(2)
+    rnd = lambda *shape: torch.randn(*shape, device=dev, generator=gen)
+    columns, first = (T + page - 1) // page, (T - n) // page
+    live = columns - first
+    table = torch.full((B, columns), -1, dtype=torch.int32, device=dev)
+    table[:, first:] = torch.randperm(B * live, device=dev, generator=gen).view(B, live).int()
+    Kp, Vp = (rnd(B * live, Hkv, page, d).to(torch.bfloat16) for _ in range(2))
+    c = torch.cumsum(torch.nn.functional.softplus(rnd(B, H, live * page) - 2.0), dim=-1).view(B, H, live, page)
+    cp = torch.empty(B * live, H, page, dtype=torch.float32, device=dev)
+    cp[table[:, first:].long()] = c.transpose(1, 2)
+    x = rnd(B, H + 2 * Hkv, d).to(torch.bfloat16)
+    weight = torch.ones(d, device=dev)
+    freq = 10000.0 ** (-torch.arange(d // 2, dtype=torch.float64, device=dev) * 2 / d)
+    alpha = torch.nn.functional.softplus(rnd(B, H) - 2.0)
+    start = torch.arange(B + 1, dtype=torch.int32, device=dev)
+    pos = torch.full((B,), T - 1, dtype=torch.int32, device=dev)
+    Q, o = (torch.empty(B, H, d, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    L = torch.empty(B, H, device=dev)
+    ws = torch.empty(g.gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, columns, w), dtype=torch.uint8, device=dev)
+    algo = B * Hkv * n * d * 2 * 2 + B * H * n * 4 + B * H * (2 * d * 2 + 4)  # window of K, V and c, the query, the output and L
+
+    def step():
+        g.gfwa_append_paged(x[:, H:H + Hkv], x[:, H + Hkv:], Kp, Vp, start, pos, table, q=x[:, :H], wq=weight, wk=weight, freq=freq, alpha=alpha, cp=cp, Q=Q)
+        g.gfwa_decode_paged(Q, Kp, Vp, cp, table, pos, w, 1.0 / d ** 0.5, o=o, L=L, workspace=ws)
+
+    for _ in range(args.warmup):
+        step()
+    torch.cuda.synchronize()
+    g.gfwa_profile_enable(True)
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        step()
+    torch.cuda.synchronize()
+    wall_ms = (time.perf_counter() - t0) / args.steps * 1e3
+    g.gfwa_profile_enable(False)
+    ms = {k: v[0] / v[1] for k, v in g.gfwa_profile_read().items() if v[1]}
+    gbs = algo / ms["decode_paged_partial"] / 1e6
+    print(json.dumps({
+        "metric": "GatedFWA decoding step on a paged cache, algorithmic GB/s of the cache-reading kernel", "value": round(gbs, 1),
+        "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(wall_ms, 5),
+        "higher_is_better": True, "dtype": "bf16", "data": "synthetic",
+        "config": {"workload": f"append and decode: B={B} H={H} Hkv={Hkv} T={T} d={d} w={w} bf16 cache in pages of {page}, all positions T-1"},
+        "roofline": {"kernel": "decode_paged_partial", "bound": "hbm", "achieved": round(gbs, 1), "peak": PEAK_HBM_GBS,
+                     "unit": "GB/s", "frac": round(gbs / PEAK_HBM_GBS, 4), "traffic": None},
+        "detail": {**{k + "_ms": round(v, 5) for k, v in ms.items()}, "algorithmic_bytes": algo,
+                   "tokens_per_s": round(B / (wall_ms * 1e-3), 1)}}))
+    return 0
+
+
 def main() -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -233,6 +287,9 @@ def main() -> int:
                     help="time the decoding step (one query per head against the cached window, bf16 cache, every "
                          "sequence at position T-1) and print its GB/s on the window's bytes instead of the usual "
                          "line, e.g. 64,32,8,16384,128,1024")
+    ap.add_argument("--paged", type=int, default=0, metavar="PAGE",
+                    help="with --decode: a serving step on a paged cache with pages of this many tokens, append of the new tokens "
+                         "(norm and rotation on the way) and decoding step")
     args = ap.parse_args()
     if args.gpus != 1:
         print("bench.py: this build runs on exactly one GPU (the path has no inter-GPU part); "
@@ -253,7 +310,7 @@ def main() -> int:
     if args.gate_only:
         return gate_only(args, g, torch)
     if args.decode:
-        return decode_only(args, g, torch)
+        return decode_paged_only(args, g, torch) if args.paged else decode_only(args, g, torch)
     wl = gi.WORKLOADS[args.workload]
     ins = {t: gi.make_tensor(wl, t) for t in ("Q", "K", "V", "alpha", "dO")} if wl.backward else gi.make_inputs(wl)
     bf = wl.dtype == "bf16"

@@ -2,7 +2,9 @@
  * gfwa_layer.h -- the operators that an attention layer of a model has directly around the calls of gfwa.h: from its
  * projection's output to the Q, K, V that the attention reads, back again for training, and the same work on a paged
  * key/value cache for serving.  Part of libgfwa; the conventions of gfwa.h hold (device pointers, the caller's stream,
- * status codes, nothing allocated, nothing launched on an error) except where a strided layout is named.
+ * status codes, nothing allocated, nothing launched on an error) except where a strided layout is named.  "Overlap" is judged by
+ * the range of bytes that a tensor spans, GFWA_ERR_OVERLAP.  A workspace belongs to its call until that is done on the stream: calls that
+ * may run at the same time (two streams, two captured graphs) need one each.
  */
 #ifndef GFWA_LAYER_H
 #define GFWA_LAYER_H
@@ -60,8 +62,8 @@ size_t gfwa_qk_norm_rope_backward_workspace_bytes(int B, int H, int Hkv, int N, 
  *
  * q, k, wq, wk, eps, freq, rot, pos, flags: as given to gfwa_qk_norm_rope; q and k are read with GFWA_HEAD_NORM only and may be
  * NULL without it.  dQ: [B,H,N,d], dK, dV: [B,Hkv,N,d] of dtype `dt`, dense, as gfwa_backward_gqa writes them.
- * dq: [B,N,H,d], dk, dv: [B,N,Hkv,d] of dtype `dt`, strided, out (views of one packed gradient, say); dV and dv are both NULL or
- * both given.  They may not overlap the inputs.  dwq, dwk: [d] fp32, out; each may be NULL; with GFWA_HEAD_NORM only (without it they
+ * dq: [B,N,H,d], dk, dv: [B,N,Hkv,d] of dtype `dt`, strided, out (views of one packed gradient, say: their rows may interleave, but
+ * share no element); dV and dv are both NULL or both given.  They may not overlap the inputs.  dwq, dwk: [d] fp32, out; each may be NULL; with GFWA_HEAD_NORM only (without it they
  * have to be NULL).  They are summed in an order that the sizes and the device alone decide.  workspace: device scratch of
  * at least gfwa_qk_norm_rope_backward_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after; may
  * be NULL where dwq and dwk are.
@@ -77,7 +79,7 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfw
  * multiple of 16.  table: [B,max_pages] int32 in device memory; position p of sequence b stands in row p % page of page
  * table[b, p / page].  Sequences may share pages that nothing appends to.  A table entry outside 0 .. pages-1 says that the
  * page is not there (a window has left it behind, or it was never given): nothing is read from it or written to it.
- * pages * heads * page * d may pass 2^31.
+ * pages * heads * page * d may pass 2^31; max_pages * page (positions) may not, nor B * H 2^22.
  */
 
 /*
@@ -111,7 +113,8 @@ int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t
  *   o   = sum_i softmax_i(S_i) v_i              L = log sum_i exp(S_i)
  *
  * q: [B,H,d] of dtype `dt`, dense.  pos: [B] int32 in device memory; a position past the table is taken as its last one.  pos[b] < 0,
- * or a page of position p that is not there: the sequence has no token, o = 0 and L = -inf.
+ * or a page of position p that is not there: the sequence has no token, o = 0 and L = -inf; so it is where every score is minus
+ * infinity (scores below -2e38 count as that).
  * o: [B,H,d] of dtype `dt`, out.  L: [B,H] fp32 out, may be NULL.  workspace: device scratch of at least
  * gfwa_decode_paged_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after.
  * Only the window is read: 2 * min(w, p+1) * d cache elements per key/value head, once for up to 16 query heads.

@@ -50,10 +50,10 @@ static int check_rotation(int dt, float eps, int rot, int flags, int d) {
     return GFWA_OK;
 }
 
-// positions are 32-bit, offsets into the cache 64-bit
+// positions are 32-bit, offsets into the cache 64-bit; a launch holds less than 2^32 threads
 static int check_cache(int B, int H, int pages, int page, int max_pages) {
     if (B <= 0 || pages <= 0 || page <= 0 || page % 16 != 0 || max_pages <= 0) return GFWA_ERR_DIM;
-    if ((long long)B * H > (1LL << 24) || (long long)max_pages * page > 0x7fffffffLL) return GFWA_ERR_DIM;
+    if ((long long)B * H > (1LL << 22) || (long long)max_pages * page > 0x7fffffffLL) return GFWA_ERR_DIM;
     return GFWA_OK;
 }
 
@@ -378,6 +378,7 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfw
         for (const Bytes& g : grads)
             if (o.bytes(B, N, d, size).meets(g)) return GFWA_ERR_OVERLAP;
     }
+    if (dwq && dwk && overlap(dwq, (size_t)d * 4, dwk, (size_t)d * 4)) return GFWA_ERR_OVERLAP;
     if (dwq || dwk) {
         if (!workspace || workspace_bytes < gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d)) return GFWA_ERR_WORKSPACE;
         if (!aligned(workspace, 16)) return GFWA_ERR_ALIGN;

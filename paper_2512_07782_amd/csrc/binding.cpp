@@ -488,7 +488,7 @@ struct Rotation {
         const int norm = PyObject_IsTrue(a[4]), paired = PyObject_IsTrue(a[5]);
         if (norm < 0 || paired < 0) throw PyError{};
         flags = (norm ? GFWA_HEAD_NORM : 0) | (paired ? GFWA_ROPE_PAIRED : 0);
-        if (!norm && (wq != nullptr || wk != nullptr)) fail(PyExc_ValueError, "wq and wk are weights of the norm, which norm=False leaves out");
+        if (!norm && (a[0] != Py_None || a[1] != Py_None)) fail(PyExc_ValueError, "wq and wk are weights of the norm, which norm=False leaves out");
     }
 };
 
@@ -573,13 +573,13 @@ PyObject* qk_norm_rope_backward(PyObject* const* a) {
     const void* pos = optional_input(a[11], ps, at::kInt, dev, "pos");
     for (int i = 15; i < 18; ++i)
         if (a[i] != Py_None) dev.also(tensor_of(a[i], "an output"), "an output");
-    const bool wants[2] = {how.wq != nullptr || a[15] != Py_None, how.wk != nullptr || a[16] != Py_None};
+    const bool wants[2] = {a[5] != Py_None || a[15] != Py_None, a[6] != Py_None || a[16] != Py_None};
     if (!(how.flags & GFWA_HEAD_NORM) && (wants[0] || wants[1])) fail(PyExc_ValueError, "dwq and dwk belong to the norm, which norm=False leaves out");
-    if (dV == nullptr && a[14] != Py_None) fail(PyExc_ValueError, "dv without dV");
+    if (a[4] == Py_None && a[14] != Py_None) fail(PyExc_ValueError, "dv without dV");
     dev.is_current();
     HeadsOutput dq(a[12], qs, st, dev, "dq"), dk(a[13], ks, st, dev, "dk");
     std::optional<HeadsOutput> dv;
-    if (dV != nullptr) dv.emplace(a[14], ks, st, dev, "dv");
+    if (a[4] != Py_None) dv.emplace(a[14], ks, st, dev, "dv");
     std::optional<Output> dw[2];
     for (int i = 0; i < 2; ++i)
         if (wants[i]) dw[i].emplace(a[15 + i], ws, at::kFloat, dev.device, i ? "dwk" : "dwq");

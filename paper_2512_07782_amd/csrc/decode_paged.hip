@@ -11,7 +11,7 @@ namespace gfwa {
 namespace {
 
 constexpr int kUnit = 16;       // positions of a unit; pages are multiples of it
-constexpr float kNone = -1.0e30f;
+constexpr float kNone = -3.0e38f;  // reference of no key yet: finite, so that differences of references are numbers, and below every score that counts
 
 // Partial result of one (query head, chunk): D output columns (not yet divided by the sum), the exponent they are scaled
 // by (log2 domain) and the sum.

@@ -359,7 +359,8 @@ def decode_check(g, dtype, q, tq, Kp, Vp, cp, tK, tV, tc, table, pos, w, **kw):
     n = count[:, None]
     rel = 2 * E + (n + 16) * U
     tol = HALF[dtype] * np.abs(o_ref) + (rel + (2 * HALF["bf16"] if dtype == "bf16" else 0))[..., None] * absv
-    err, lerr = np.abs(host(o) - o_ref), host(L) - L_ref
+    with np.errstate(invalid="ignore"):  # empty rows: minus infinity on both sides
+        err, lerr = np.abs(host(o) - o_ref), host(L) - L_ref
     empty = np.isinf(L_ref)
     assert np.array_equal(np.isinf(host(L)), empty) and (host(o)[empty] == 0).all()
     assert (err <= tol + 1e-30).all(), (err / (tol + 1e-30)).max()
@@ -448,6 +449,31 @@ def test_decode_masked_keys_and_scores_far_apart(g, H, Hkv, dtype):
     decode_check(g, dtype, q, tq, K3, V3, cp, tK3, tV3, gpu(cp), table, [T - 5] * 2, w)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [40, 2500])
+def test_decode_masked_keys_with_finite_scores(g, T, dtype):
+    """Where every key holds the type's lowest value and the query little there, scores are of the order of -1e37, all equal in 32 bits: weights
+    are even, not none.  With one key unmasked it has all the weight."""
+    H, Hkv, page, d = 4, 2, 16, 64
+    rng, table, Kp, Vp, cp = paged_case(7, [(T, 0)], H, Hkv, d, page, dtype)
+    q, tq = store(np.concatenate([np.full((1, H, 1), 0.25), rng.standard_normal((1, H, d - 1))], -1), dtype)
+    low = torch.finfo(TORCH[dtype]).min
+    Kp[..., 0] = np.where(np.isnan(Kp[..., 0]), np.nan, low)
+    (K1, tK), (V1, tV) = store(Kp, dtype), store(Vp, dtype)
+    pos = torch.tensor([T - 1], dtype=torch.int32, device=DEV)
+    o, L = g.gfwa_decode_paged(tq, tK, tV, gpu(cp), gpu(table), pos, 1 << 30, 0.125)
+    i = np.arange(T)
+    V = V1[table[0, i // page], :, i % page].astype(np.float64)
+    mean = np.repeat(V.mean(0), H // Hkv, 0)
+    # even weights: sums of T terms and the rounding of the result, in bf16 of the weights too (1 is exact in it)
+    assert (np.abs(host(o)[0] - mean) <= HALF[dtype] * np.abs(mean) + (T + 16) * U * np.abs(V).mean(0).max()).all()
+    assert np.allclose(host(L), 0.125 * 0.25 * float(low), rtol=1e-6)
+    Kp[table[0, 3 // page], :, 3 % page, 0] = 0.0
+    o, L = g.gfwa_decode_paged(tq, store(Kp, dtype)[1], tV, gpu(cp), gpu(table), pos, 1 << 30, 0.125)
+    one = np.repeat(V[3], H // Hkv, 0)
+    assert (np.abs(host(o)[0] - one) <= HALF[dtype] * np.abs(one)).all() and np.isfinite(host(L)).all() and (host(L) > -1e6).all()
+
+
 def test_decode_clamps_positions_past_the_table(g):
     rng, table, Kp, Vp, cp = paged_case(3, [(64, 0)] * 3, 4, 2, 64, 16, "bf16", M=4)
     q, tq = store(rng.standard_normal((3, 4, 64)), "bf16")
@@ -480,6 +506,58 @@ def test_caches_beyond_32_bit_offsets(g):
     assert torch.isfinite(outs[0][1]).all()
     for a, b in zip(*outs):
         assert torch.equal(a, b)
+
+
+def test_rows_beyond_32_bit_offsets(g):
+    """Projections and head-major tensors of more than 2^31 elements: the last rows are those of a small call."""
+    N, H, Hkv, d = 132000, 112, 8, 128
+    x = torch.empty((1, N, H + 2 * Hkv, d), dtype=torch.bfloat16, device=DEV).normal_()
+    assert x.numel() > 1 << 31
+    wt, f = 1 + 0.1 * torch.randn(d, device=DEV), dev64(freq_of(d))
+    split = lambda t: (t[:, :, :H], t[:, :, H:H + Hkv], t[:, :, H + Hkv:])
+    pos = torch.arange(N, dtype=torch.int32, device=DEV)[None]
+    Q, K, V = g.gfwa_qk_norm_rope(*split(x), wt, wt, freq=f)
+    n = 100
+    tail = x[:, -n:].contiguous()
+    for a, b in zip((Q, K, V), g.gfwa_qk_norm_rope(*split(tail), wt, wt, freq=f, pos=pos[:, -n:].contiguous())):
+        assert torch.equal(a[:, :, -n:], b)
+    dx = torch.empty_like(x)
+    dq, dk, dv = split(dx)
+    g.gfwa_qk_norm_rope_backward(*split(x)[:2], Q, K, V, wt, wt, freq=f, dq=dq, dk=dk, dv=dv)
+    got = g.gfwa_qk_norm_rope_backward(*split(tail)[:2], Q[:, :, -n:].contiguous(), K[:, :, -n:].contiguous(), V[:, :, -n:].contiguous(), wt, wt, freq=f,
+                                       pos=pos[:, -n:].contiguous())
+    for a, b in zip((dq, dk, dv), got):
+        assert torch.equal(a[:, -n:], b)
+
+
+def test_append_past_the_table_and_from_unaligned_vectors(g):
+    """Positions that the table has no column for are not written, their queries are; vectors may start at any multiple of their own size."""
+    lens = [(30, 20), (0, 40)]
+    rng, table, Kp, Vp, cp = paged_case(8, lens, 4, 2, 64, 16, "f32", M=2)
+    start, cached = np.array([0, 20, 60], dtype=np.int32), np.array([30, 0], dtype=np.int32)
+    q, k, v = (store(rng.standard_normal((60, h, 64)), "f32") for h in (4, 2, 2))
+    alpha = (rng.random((60, 4)) * 0.3).astype(np.float32)
+    wt = (1 + 0.3 * rng.standard_normal(64)).astype(np.float32)
+
+    def odd(x):  # the same values one element into a buffer
+        b = torch.zeros(x.size + 1, dtype=torch.from_numpy(x).dtype, device=DEV)
+        b[1:] = gpu(x).flatten()
+        return b[1:].view(x.shape)
+
+    tK, tV, tc, tQ = store(Kp, "f32")[1], store(Vp, "f32")[1], odd(cp), torch.zeros((60, 4, 64), device=DEV)
+    freq = freq_of(64)
+    g.gfwa_append_paged(k[1], v[1], tK, tV, odd(start), odd(cached), odd(table), q=q[1], wq=odd(wt), wk=odd(wt), eps=EPS, freq=odd(freq), alpha=odd(alpha),
+                        cp=tc, Q=tQ)
+    Qr, Kr, Vr, cr = ol.append_paged(q[0], k[0], v[0], wt, wt, EPS, True, freq, False, alpha, start, cached, table, np.zeros((60, 4, 64)), Kp, Vp, cp)
+    for got, ref in ((tK, Kr), (tV, Vr), (tc, cr), (tQ, Qr)):
+        got = host(got)
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+        fin = ~np.isnan(ref)
+        assert (np.abs(got[fin] - ref[fin]) <= 128 * U * max(1, np.abs(ref[fin]).max())).all()
+    pos = np.array([31, 31], dtype=np.int32)
+    o, L = g.gfwa_decode_paged(tQ[[1, 51]].contiguous(), tK, tV, tc, odd(table), odd(pos), 20, 0.125)
+    o1, L1 = g.gfwa_decode_paged(tQ[[1, 51]].contiguous(), tK, tV, tc.clone(), gpu(table), gpu(pos), 20, 0.125)
+    assert torch.equal(o, o1) and torch.equal(L, L1) and torch.isfinite(o).all()
 
 
 # ---- as they are used
@@ -637,3 +715,17 @@ def test_two_streams_at_once(g):
     for a, many in zip(alone, outs):
         for got in many:
             assert all(torch.equal(x, y) for x, y in zip(a, got))
+
+
+def test_bench_line_of_the_paged_step(g, capsys):
+    import json
+    import sys
+    import bench
+    argv, sys.argv = sys.argv, ["bench.py", "--decode", "3,8,2,700,64,100", "--paged", "16", "--steps", "3", "--warmup", "1"]
+    try:
+        assert bench.main() == 0
+    finally:
+        sys.argv = argv
+    line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert line["unit"] == "GB/s" and line["value"] > 0 and line["steps"] == 3
+    assert {"append_paged_ms", "decode_paged_partial_ms", "algorithmic_bytes", "tokens_per_s"} <= set(line["detail"])

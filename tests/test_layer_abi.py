@@ -78,7 +78,7 @@ def rope_bwd(lib, **kw):
     outs = [r(kw.get("dq", heads(0x8000000, 5120, 512, 64))), r(kw.get("dk", heads(0x8000000 + 512, 5120, 512, 64))),
             r(kw.get("dv", heads(0x8000000 + 768, 5120, 512, 64)))]
     return lib.gfwa_qk_norm_rope_backward(kw.get("dt", 0), *ins, A, A, kw.get("eps", 1e-6), A, kw.get("rot", 64), None, kw.get("flags", 1),
-                                          kw.get("dQ", P(0x2000000)), P(0x3000000), kw.get("dV", P(0x4000000)), *outs, kw.get("dwq", A), kw.get("dwk", A),
+                                          kw.get("dQ", P(0x2000000)), P(0x3000000), kw.get("dV", P(0x4000000)), *outs, kw.get("dwq", A), kw.get("dwk", P(0x20000)),
                                           kw.get("ws", P(0x5000000)), kw.get("wsb", 1 << 30), 2, 4, kw.get("Hkv", 2), 10, kw.get("d", 64), None)
 
 
@@ -87,7 +87,7 @@ def rope_bwd(lib, **kw):
     (-2, dict(Hkv=3)), (-2, dict(rot=24)), (-2, dict(eps=-1.0)), (-3, dict(d=32)), (-3, dict(dt=5)), (-3, dict(flags=0)), (-3, dict(flags=8)),
     (-4, dict(dQ=P(0x2000004))), (-4, dict(dwq=P(0x10001))), (-4, dict(dq=heads(0x8000004, 5120, 512, 64))), (-4, dict(ws=P(0x5000008))),
     (-5, dict(ws=None)), (-5, dict(wsb=1000)),
-    (-7, dict(dq=heads(0x1000000, 5120, 512, 64))), (-7, dict(dq=heads(0x2000000, 5120, 512, 64))),
+    (-7, dict(dwk=A)), (-7, dict(dwk=P(0x10000 + 128))), (-7, dict(dq=heads(0x1000000, 5120, 512, 64))), (-7, dict(dq=heads(0x2000000, 5120, 512, 64))),
     (-7, dict(dq=heads(0x8000000, 0, 512, 64))), (-7, dict(dq=heads(0x8000000, 5120, 128, 64))), (-7, dict(dq=heads(0x8000000, 5120, 512, 0))),
 ])
 def test_rope_backward_refuses(lib, status, kw):
@@ -132,7 +132,7 @@ def decode(lib, **kw):
 
 @pytest.mark.parametrize("status,kw", [
     (-1, dict(q=None)), (-1, dict(cp=None)), (-1, dict(table=None)), (-1, dict(pos=None)), (-1, dict(o=None)),
-    (-2, dict(B=0)), (-2, dict(Hkv=3)), (-2, dict(pages=-1)), (-2, dict(page=20)), (-2, dict(M=0)), (-2, dict(w=0)), (-2, dict(M=1 << 27)),
+    (-2, dict(B=0)), (-2, dict(Hkv=3)), (-2, dict(pages=-1)), (-2, dict(page=20)), (-2, dict(M=0)), (-2, dict(w=0)), (-2, dict(M=1 << 27)), (-2, dict(B=1 << 21)),
     (-3, dict(d=96)), (-3, dict(dt=9)), (-4, dict(q=P(0x10008))), (-4, dict(o=P(0x10008))), (-4, dict(L=P(0x10002))), (-4, dict(pos=P(0x10001))), (-4, dict(ws=P(0x10008))),
     (-5, dict(ws=None)), (-5, dict(wsb=8)),
 ])
