@@ -102,7 +102,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
 #pragma unroll
     for (int i = 0; i < 32; ++i) sums[wv][i >> 4][i & 15][lane] = 0.f;
     struct Rows {
-        LaneRow<T, D, ONCE> g, x;
+        LaneRow<T, D, ONCE> g;  // (the inputs past the caches too: 127 us against 123 at H 32, Hkv 8, N 16384, d 128)
+        LaneRow<T, D> x;
     };
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
@@ -219,13 +220,17 @@ __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __re
     }
 }
 
-constexpr int kMostSums = 2048;  // workgroups that leave sums of the weights' gradients
+// Workgroups that leave sums of the weights' gradients: three waves a SIMD are there at a time (bf16), and what fits in them goes at once; more goes through
+// two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 120 / 123, B 4, H 16, N 8192 208 /
+// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 27 / 23 / 23).
+constexpr int kMostSums = 768, kManySums = 512;
 
-long long share_out(RopeArgs& a, int D, long long most) {
+long long share_out(RopeArgs& a, int D) {
     const int side = D == 128 ? kSide<128> : kSide<64>;
     a.shares = Shares((int)(((long long)a.tokens * side + 1024 / D - 1) / (1024 / D)), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
     const long long blocks = ((long long)a.shares.items + kRopeWaves - 1) / kRopeWaves;
-    return blocks < most ? blocks : most;
+    if (a.part != nullptr) return blocks <= kMostSums ? blocks : kManySums;
+    return blocks < 1 << 20 ? blocks : 1 << 20;
 }
 
 }  // namespace
@@ -258,7 +263,7 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.q = q;
     a.k = k;
     a.v = v;
-    const long long blocks = share_out(a, d, 1 << 20);
+    const long long blocks = share_out(a, d);
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
     if (bf16) {
@@ -281,7 +286,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.x_q = q;
     a.x_k = k;
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
-    const long long blocks = share_out(a, d, a.part != nullptr ? kMostSums : 1 << 20);
+    const long long blocks = share_out(a, d);
     {
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
