@@ -162,7 +162,8 @@ template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
     if ((int)blockIdx.x < a.scan_blocks) {
-        const long long i = (long long)blockIdx.x * kAppendWaves + (threadIdx.x >> 6);
+        // the heads of a sequence on one XCD: they read the same lines of alpha
+        const long long i = (long long)xcd_remap(blockIdx.x, a.scan_blocks) * kAppendWaves + (threadIdx.x >> 6);
         const int units = (a.H + a.scan_heads - 1) / a.scan_heads;
         if (i < (long long)a.B * units) prefix_of(a, (int)(i / units), (int)(i % units) * a.scan_heads, a.scan_heads);
         return;

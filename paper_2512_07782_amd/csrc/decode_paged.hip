@@ -13,6 +13,8 @@ namespace {
 constexpr int kUnit = 16;       // positions of a unit; pages are multiples of it
 constexpr float kNone = -3.0e38f;  // reference of no key yet: finite, so that differences of references are numbers, and below every score that counts
 
+constexpr int kFewChunks = 16;
+
 // Partial result of one (query head, chunk): D output columns (not yet divided by the sum), the exponent they are scaled
 // by (log2 domain) and the sum.
 __host__ __device__ constexpr int record(int D) { return D + 2; }
@@ -248,7 +250,14 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
     // the tiles of this chunk, counted from the newest unit back
     const int u_hi = me.p / kUnit, u_lo = me.lo / kUnit;
     const int t1 = me.page < 0 ? 0 : min((s + 1) * a.chunk, (u_hi - u_lo) / NU + 1);
-    if (a.splits > 1 && s * a.chunk >= t1) return;  // the merge knows
+    if (a.splits > 1 && s * a.chunk >= t1) {  // nothing of the window here
+        if (a.splits <= kFewChunks && (int)threadIdx.x < GT) {
+            float* rec = a.part + (((size_t)b * a.H + h0 + threadIdx.x) * a.splits + s) * record(D);
+            rec[D] = kNone;
+            rec[D + 1] = 0.f;
+        }
+        return;
+    }
     int t = s * a.chunk + wv;
     if (t < t1) {
         const T* const K = (const T*)a.Kp + (size_t)kvh * a.page * D;
@@ -384,15 +393,20 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
 }
 
 // o = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  L = (M + log2 of that sum) ln 2
-// over the chunks that hold part of the window (the others write nothing).  NG groups of D threads take every NG-th record each.
+// over the chunks.  NG groups of D threads take every NG-th record each.  Up to kFewChunks every chunk leaves a record, without sums where it holds
+// nothing of the window; of more than that only those that do, and the merge looks up which (one conversation, w 1024, nine chunks: 0.3 us
+// less without the look; whole sequences, 65 chunks: 3 us more).
 template <typename T, int D, int NG>
 __global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const PagedArgs a) {
     __shared__ float sm_o[NG][D], sm_m[NG], sm_l[NG];
     const size_t bh = blockIdx.x;
     const int col = threadIdx.x % D, grp = threadIdx.x / D;
-    const Query me(a, (int)(bh / a.H));
-    const int pieces = me.page < 0 ? 0 : (me.p / kUnit - me.lo / kUnit) / Tile<T, D>::kUnits + 1;
-    const int there = (pieces + a.chunk - 1) / a.chunk;
+    int there = a.splits;
+    if (NG > 1) {
+        const Query me(a, (int)(bh / a.H));
+        const int pieces = me.page < 0 ? 0 : (me.p / kUnit - me.lo / kUnit) / Tile<T, D>::kUnits + 1;
+        there = (pieces + a.chunk - 1) / a.chunk;
+    }
     const float* rec = a.part + bh * a.splits * record(D);
     float mm = kNone, ll = 0.f, oo = 0.f;
     constexpr int U = 8;  // records whose loads are in flight together
@@ -415,7 +429,7 @@ __global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const Page
         for (int u = 0; u < U; ++u) {
             const float f = s0 + u * NG < there ? fast_exp2(m[u] - mn) : 0.f;
             ll = fmaf(l[u], f, ll);
-            oo = fmaf(x[u], f, oo);
+            oo = l[u] == 0.f ? oo : fmaf(x[u], f, oo);  // (no weight, no sums: an infinity there stays out)
         }
         mm = mn;
     }
@@ -505,7 +519,7 @@ static hipError_t launch(const PagedArgs& given, int B, hipStream_t s) {
     }
     if (a.splits > 1) {
         ProfScope prof(kKernDecodePagedCombine, s);
-        if (a.splits > 16) hipLaunchKernelGGL((decode_paged_combine_kernel<T, D, 4>), dim3(B * a.H), dim3(4 * D), 0, s, a);
+        if (a.splits > kFewChunks) hipLaunchKernelGGL((decode_paged_combine_kernel<T, D, 4>), dim3(B * a.H), dim3(4 * D), 0, s, a);
         else hipLaunchKernelGGL((decode_paged_combine_kernel<T, D, 1>), dim3(B * a.H), dim3(D), 0, s, a);
     }
     return hipGetLastError();
