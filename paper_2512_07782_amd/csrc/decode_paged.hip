@@ -27,24 +27,39 @@ struct PagedArgs {
     float *L, *part;
     int H, Hkv, pages, page, max_pages, w;
     float scale;
-    int splits, chunk;  // chunks of the window and tiles of one
+    int splits, waves;  // chunks a window may be cut into, and waves of a workgroup
+    int least, chunk;   // tiles of a chunk: at least, and at most
     int items;          // workgroups of one chunk
     int units_shift;    // log2 of the units of a page, -1: no power of two
 };
 
-// A sequence's query position and what of its prefix and window is there.
+// Tiles of a chunk of a window of `tiles`: what the longest window is cut into; but a sequence of less than an eighth of that (a table has columns
+// for the longest one there may be) is cut into all the chunks there are, none smaller than the least.  (Eight sequences of 1000 tokens, H 32, Hkv 8,
+// d 128, without a window in a table for 131072: 21.8 us in one chunk each, 11.7 in five.  Every sequence like that: 16 of up to 8192 in fp32 126 us
+// against 123.)
+__device__ __forceinline__ int chunk_of(const PagedArgs& a, int tiles) {
+    if (tiles >= a.chunk * (long long)a.splits / 8) return a.chunk;
+    const int c = ((tiles + a.splits - 1) / a.splits + a.waves - 1) / a.waves * a.waves;
+    return min(max(c, a.least), a.chunk);
+}
+
+// A sequence's query position, the first position of its window, and once looked up the page and row that hold the query position.
 struct Query {
-    int p, lo, page, row;  // page -1: no token
+    int p, lo, page = -1, row = 0;  // p < 0, or page -1: no token
     __device__ __forceinline__ Query(const PagedArgs& a, int b) {
         p = min(a.pos[b], a.max_pages * a.page - 1);
-        page = -1;
-        row = lo = 0;
+        lo = p < 0 ? 0 : max(0, p - a.w + 1);
+    }
+    // tiles of U units that the window touches
+    template <int U>
+    __device__ __forceinline__ int tiles() const {
+        return p < 0 ? 0 : (p / kUnit - lo / kUnit) / U + 1;
+    }
+    __device__ __forceinline__ void look_up(const PagedArgs& a, int b) {
         if (p < 0) return;
-        const int i = p / a.page;
+        const int i = p / a.page, id = a.table[(size_t)b * a.max_pages + i];
         row = p - i * a.page;
-        const int id = a.table[(size_t)b * a.max_pages + i];
         if (id >= 0 && id < a.pages) page = id;
-        lo = max(0, p - a.w + 1);
     }
 };
 
@@ -239,7 +254,17 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
     const int GT = min(kHeads, G - gc * kHeads), h0 = kvh * G + gc * kHeads;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hd = lane & 15, g = lane >> 4, head = h0 + min(hd, GT - 1);
-    const Query me(a, b);
+    Query me(a, b);
+    const int tiles = me.tiles<NU>(), chunk = chunk_of(a, tiles);
+    if (a.splits > 1 && s * chunk >= tiles) {  // nothing of the window here
+        if (a.splits <= kFewChunks && (int)threadIdx.x < GT) {
+            float* rec = a.part + (((size_t)b * a.H + h0 + threadIdx.x) * a.splits + s) * record(D);
+            rec[D] = kNone;
+            rec[D + 1] = 0.f;
+        }
+        return;
+    }
+    me.look_up(a, b);
 
     f32x4 acc[Tl::DT];
 #pragma unroll
@@ -249,16 +274,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
 
     // the tiles of this chunk, counted from the newest unit back
     const int u_hi = me.p / kUnit, u_lo = me.lo / kUnit;
-    const int t1 = me.page < 0 ? 0 : min((s + 1) * a.chunk, (u_hi - u_lo) / NU + 1);
-    if (a.splits > 1 && s * a.chunk >= t1) {  // nothing of the window here
-        if (a.splits <= kFewChunks && (int)threadIdx.x < GT) {
-            float* rec = a.part + (((size_t)b * a.H + h0 + threadIdx.x) * a.splits + s) * record(D);
-            rec[D] = kNone;
-            rec[D + 1] = 0.f;
-        }
-        return;
-    }
-    int t = s * a.chunk + wv;
+    const int t1 = me.page < 0 ? 0 : min((s + 1) * chunk, tiles);
+    int t = s * chunk + wv;
     if (t < t1) {
         const T* const K = (const T*)a.Kp + (size_t)kvh * a.page * D;
         const T* const V = (const T*)a.Vp + (size_t)kvh * a.page * D;
@@ -394,7 +411,7 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
 
 // o = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  L = (M + log2 of that sum) ln 2
 // over the chunks.  NG groups of D threads take every NG-th record each.  Up to kFewChunks every chunk leaves a record, without sums where it holds
-// nothing of the window; of more than that only those that do, and the merge looks up which (one conversation, w 1024, nine chunks: 0.3 us
+// nothing of the window; of more than that only those that do, and the merge asks for the position (one conversation, w 1024, nine chunks: 0.3 us
 // less without the look; whole sequences, 65 chunks: 3 us more).
 template <typename T, int D, int NG>
 __global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const PagedArgs a) {
@@ -404,8 +421,8 @@ __global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const Page
     int there = a.splits;
     if (NG > 1) {
         const Query me(a, (int)(bh / a.H));
-        const int pieces = me.page < 0 ? 0 : (me.p / kUnit - me.lo / kUnit) / Tile<T, D>::kUnits + 1;
-        there = (pieces + a.chunk - 1) / a.chunk;
+        const int tiles = me.template tiles<Tile<T, D>::kUnits>(), chunk = chunk_of(a, tiles);
+        there = (tiles + chunk - 1) / chunk;
     }
     const float* rec = a.part + bh * a.splits * record(D);
     float mm = kNone, ll = 0.f, oo = 0.f;
@@ -467,7 +484,8 @@ int most_units(int page, int max_pages, int w) {
 // How a step is cut up; follows from the sizes alone, as the workspace does.
 struct Plan {
     int waves;          // of a workgroup
-    int chunk, splits;  // tiles of a chunk, chunks
+    int chunk, splits;  // tiles of a chunk of the longest window, chunks
+    int least;          // tiles of a chunk of shorter ones
     long long items;    // workgroups of one chunk
     Plan(bool bf16, int B, int H, int Hkv, int page, int max_pages, int w) {
         const int G = H / Hkv, units = most_units(page, max_pages, w), of = bf16 ? Tile<bf16_t, 128>::kUnits : Tile<float, 128>::kUnits;
@@ -483,10 +501,12 @@ struct Plan {
         //   * a window of three tiles a wave is not worth the merge (300 keys of one sequence: 4.4, in three chunks 6.3).
         const bool even = w < (long long)max_pages * page;
         long long S = 1;
+        least = waves;
         if (even && items >= 512) waves = 4;
         else if (tiles <= 24 || (even && items >= 256)) waves = 8;
         else {
-            const long long want = even ? 512 : 4096, least = even ? waves : 2 * waves;
+            const long long want = even ? 512 : 4096;
+            least = even ? waves : 2 * waves;
             S = (want + items - 1) / items;
             if (S > (tiles + least - 1) / least) S = (tiles + least - 1) / least;
         }
@@ -508,6 +528,8 @@ static hipError_t launch(const PagedArgs& given, int B, hipStream_t s) {
     const Plan plan(sizeof(T) == 2, B, a.H, a.Hkv, a.page, a.max_pages, a.w);
     a.chunk = plan.chunk;
     a.splits = plan.splits;
+    a.least = plan.least;
+    a.waves = plan.waves;
     a.items = (int)plan.items;
     {
         ProfScope prof(kKernDecodePaged, s);

@@ -58,8 +58,8 @@ struct Unit8<float> {
 };
 
 // Which elements of a row lane j (of D / 16) holds, and the rotation of them.
-//   rotation of (m, m + rot/2): the first rot / 16 lanes hold the units at 8 j and rot/2 + 8 j, the others two neighbouring units
-//   behind the rotated part;  rotation of (2m, 2m + 1): the units at 8 j and D/2 + 8 j, each rotated if it stands in front of rot.
+//   rotation of (m, m + rot/2): the first rot / 16 lanes hold the units at 8 j and rot/2 + 8 j, the others those at the same place in the two
+//   halves of what lies behind the rotated part, rot/2 + 8 j and D/2 + 8 j;  rotation of (2m, 2m + 1): the units at 8 j and D/2 + 8 j, each rotated if it stands in front of rot.
 // Either way a lane has at most eight angles.
 template <int D>
 struct LaneOfRow {
@@ -78,8 +78,8 @@ struct LaneOfRow {
             turn_b = b < rot;
         } else {
             turn_a = turn_b = 16 * j < rot;
-            a = turn_a ? 8 * j : 16 * j;
-            b = turn_a ? rot / 2 + 8 * j : 16 * j + 8;
+            a = turn_a ? 8 * j : 8 * j + rot / 2;
+            b = turn_a ? rot / 2 + 8 * j : 8 * j + D / 2;
             m = 8 * j;
             mb = m + 4;
         }

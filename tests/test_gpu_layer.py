@@ -729,3 +729,23 @@ def test_bench_line_of_the_paged_step(g, capsys):
     line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
     assert line["unit"] == "GB/s" and line["value"] > 0 and line["steps"] == 3
     assert {"append_paged_ms", "decode_paged_partial_ms", "algorithmic_bytes", "tokens_per_s"} <= set(line["detail"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Hkv,G,d", [(1, 2, 4, 128), (5, 1, 3, 64), (40, 8, 1, 64)])
+def test_decode_short_sequences_in_a_long_table(g, B, Hkv, G, d, dtype):
+    """Columns for 65536 positions, sequences of up to a few hundred: the steps of a table that just holds them, to the order of the sums."""
+    page, H = 16, Hkv * G
+    rng, table, Kp, Vp, cp = paged_case(11, [(int(n), 0) for n in np.random.default_rng(B).integers(1, 500, B)], H, Hkv, d, page, dtype)
+    lens = [int((~np.isnan(cp[table[b], 0])).sum()) for b in range(B)]
+    q, tq = store(rng.standard_normal((B, H, d)), dtype)
+    (K1, tK), (V1, tV), tc = store(Kp, dtype), store(Vp, dtype), gpu(cp)
+    wide = np.full((B, 4096), -1, dtype=np.int32)
+    wide[:, :table.shape[1]] = table
+    pos = [n - 1 for n in lens]
+    decode_check(g, dtype, q, tq, K1, V1, cp, tK, tV, tc, table, pos, 1 << 30)
+    decode_check(g, dtype, q, tq, K1, V1, cp, tK, tV, tc, wide, pos, 1 << 30)
+    # ... and one position at the far end among them: a window over the sequence's first tokens, seen there
+    n = min(lens[0], 38)
+    wide[0, -3:] = np.resize(table[0], 3)
+    decode_check(g, dtype, q, tq, K1, V1, cp, tK, tV, tc, wide, [65536 - 48 + n - 1] + pos[1:], n)
