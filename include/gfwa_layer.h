@@ -2,8 +2,9 @@
  * gfwa_layer.h -- the operators that an attention layer of a model has directly around the calls of gfwa.h: from its
  * projection's output to the Q, K, V that the attention reads, back again for training, and the same work on a paged
  * key/value cache for serving.  Part of libgfwa; the conventions of gfwa.h hold (device pointers, the caller's stream,
- * status codes, nothing allocated, nothing launched on an error) except where a strided layout is named.  "Overlap" is judged by
- * the range of bytes that a tensor spans, GFWA_ERR_OVERLAP.  A workspace belongs to its call until that is done on the stream: calls that
+ * status codes, nothing allocated, nothing launched on an error) except where a strided layout is named.  What a call writes
+ * (outputs, cache, workspace) may not overlap what it reads, nor each other, judged by the ranges of bytes that the tensors span:
+ * GFWA_ERR_OVERLAP (dq, dk and dv among each other are the one exception).  A workspace belongs to its call until that is done on the stream: calls that
  * may run at the same time (two streams, two captured graphs) need one each.
  */
 #ifndef GFWA_LAYER_H
@@ -45,7 +46,7 @@ enum {
  * q: [B,N,H,d], k, v: [B,N,Hkv,d] of dtype `dt`, strided;  v may be NULL (V is then ignored).
  * wq, wk: [d] fp32 or NULL.  freq: [rot/2] fp64 in device memory, 8-byte aligned, in radians for each position; rot: a multiple of
  * 16 up to d, 0: no rotation, freq ignored.  pos: [B,N] int32 in device memory, any values; NULL: token n stands at position n.
- * Q: [B,H,N,d], K, V: [B,Hkv,N,d] of dtype `dt`, dense, out; they may not overlap the inputs.
+ * Q: [B,H,N,d], K, V: [B,Hkv,N,d] of dtype `dt`, dense, out.
  * d in {64, 128}; Hkv divides H.
  */
 int gfwa_qk_norm_rope(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t *k, const gfwa_heads_t *v, const float *wq,
@@ -63,8 +64,8 @@ size_t gfwa_qk_norm_rope_backward_workspace_bytes(int B, int H, int Hkv, int N, 
  * q, k, wq, wk, eps, freq, rot, pos, flags: as given to gfwa_qk_norm_rope; q and k are read with GFWA_HEAD_NORM only and may be
  * NULL without it.  dQ: [B,H,N,d], dK, dV: [B,Hkv,N,d] of dtype `dt`, dense, as gfwa_backward_gqa writes them.
  * dq: [B,N,H,d], dk, dv: [B,N,Hkv,d] of dtype `dt`, strided, out (views of one packed gradient, say: their rows may interleave, but
- * share no element); dV and dv are both NULL or both given.  They may not overlap the inputs.  dwq, dwk: [d] fp32, out; each may be NULL; with GFWA_HEAD_NORM only (without it they
- * have to be NULL).  They are summed in an order that the sizes and the device alone decide.  workspace: device scratch of
+ * share no element); dV and dv are both NULL or both given.  dwq, dwk: [d] fp32, out; each may be
+ * NULL; with GFWA_HEAD_NORM only (without it they have to be NULL).  They are summed in an order that the sizes and the device alone decide.  workspace: device scratch of
  * at least gfwa_qk_norm_rope_backward_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after; may
  * be NULL where dwq and dwk are.
  */
@@ -97,7 +98,7 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfw
  * start: [B+1], cached: [B] int32 in device memory, start not decreasing, cached >= 0 (a sequence may have no new token).
  * Rows that belong to no sequence (in front of start[0], from start[B] on) are left out: their rows of Q stay as they were.  Of rows whose
  * position lies outside the table, or in a page that is not there, the query alone is written.
- * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page.  Q and the cache may not overlap the inputs.
+ * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page.
  */
 int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t *k, const gfwa_heads_t *v, const float *wq,
                       const float *wk, float eps, const double *freq, int rot, int flags, const float *alpha, long long alpha_token,

@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 #include <utility>
 
@@ -62,6 +63,16 @@ struct Bytes {
     size_t count;
     bool meets(const Bytes& o) const { return at && o.at && overlap(at, count, o.at, o.count); }
 };
+// whether one of what a call writes meets another one or something that it reads
+static bool any_meet(std::initializer_list<Bytes> writes, std::initializer_list<Bytes> reads) {
+    for (const Bytes* w = writes.begin(); w != writes.end(); ++w) {
+        for (const Bytes* o = writes.begin(); o != w; ++o)
+            if (w->meets(*o)) return true;
+        for (const Bytes& r : reads)
+            if (w->meets(r)) return true;
+    }
+    return false;
+}
 
 // The strided tensor of `heads` heads that a caller describes; nullptr: none.
 struct HeadsSpan {
@@ -336,12 +347,9 @@ int gfwa_qk_norm_rope(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfwa_heads_t
     for (const Bytes& o : outs)
         if (!aligned(o.at, 16)) return GFWA_ERR_ALIGN;
     if (!aligned(wq, 4) || !aligned(wk, 4) || !aligned(pos, 4) || (rot > 0 && !aligned(freq, 8))) return GFWA_ERR_ALIGN;
-    for (int i = 0; i < 3; ++i) {
-        for (const HeadsSpan& x : spans)
-            if (outs[i].meets(x.bytes(B, N, d, size))) return GFWA_ERR_OVERLAP;
-        for (int j = 0; j < i; ++j)
-            if (outs[i].meets(outs[j])) return GFWA_ERR_OVERLAP;
-    }
+    if (any_meet({outs[0], outs[1], outs[2]}, {spans[0].bytes(B, N, d, size), spans[1].bytes(B, N, d, size), spans[2].bytes(B, N, d, size), {wq, (size_t)d * 4},
+                                               {wk, (size_t)d * 4}, {rot > 0 ? freq : nullptr, (size_t)rot * 4}, {pos, (size_t)B * N * 4}}))
+        return GFWA_ERR_OVERLAP;
     const HeadRotation how{wq, wk, eps, freq, rot, pos, (flags & GFWA_HEAD_NORM) != 0, (flags & GFWA_ROPE_PAIRED) != 0};
     return hip_status(qk_norm_rope(dt == GFWA_BF16, view(q), view(k), view(v), how, Q, K, V, B, H, Hkv, N, d, stream));
 }
@@ -378,10 +386,17 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfw
         for (const Bytes& g : grads)
             if (o.bytes(B, N, d, size).meets(g)) return GFWA_ERR_OVERLAP;
     }
-    if (dwq && dwk && overlap(dwq, (size_t)d * 4, dwk, (size_t)d * 4)) return GFWA_ERR_OVERLAP;
+    const Bytes wqs{wq, (size_t)d * 4}, wks{wk, (size_t)d * 4}, angles{rot > 0 ? freq : nullptr, (size_t)rot * 4}, positions{pos, (size_t)B * N * 4};
+    for (const HeadsSpan& o : outs)
+        if (any_meet({o.bytes(B, N, d, size)}, {wqs, wks, angles, positions})) return GFWA_ERR_OVERLAP;
     if (dwq || dwk) {
-        if (!workspace || workspace_bytes < gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d)) return GFWA_ERR_WORKSPACE;
+        const size_t scratch = gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d);
+        if (!workspace || workspace_bytes < scratch) return GFWA_ERR_WORKSPACE;
         if (!aligned(workspace, 16)) return GFWA_ERR_ALIGN;
+        if (any_meet({{dwq, (size_t)d * 4}, {dwk, (size_t)d * 4}, {workspace, scratch}},
+                     {ins[0].bytes(B, N, d, size), ins[1].bytes(B, N, d, size), grads[0], grads[1], grads[2], outs[0].bytes(B, N, d, size),
+                      outs[1].bytes(B, N, d, size), outs[2].bytes(B, N, d, size), wqs, wks, angles, positions}))
+            return GFWA_ERR_OVERLAP;
     }
     const HeadRotation how{wq, wk, eps, freq, rot, pos, norm, (flags & GFWA_ROPE_PAIRED) != 0};
     return hip_status(qk_norm_rope_backward(dt == GFWA_BF16, view(q), view(k), how, dQ, dK, dV, view(dq), view(dk), view(dv), dwq, dwk,
@@ -416,13 +431,10 @@ int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfwa_heads_t
     const size_t per_head = (size_t)pages * page;
     const Bytes outs[] = {{Q, (size_t)rows * H * d * size}, {Kp, per_head * Hkv * d * size}, {Vp, per_head * Hkv * d * size}, {cp, per_head * H * 4}};
     const Bytes gate{alpha, alpha ? 4 * (size_t)((rows - 1) * alpha_token + (H - 1) * alpha_head + 1) : 0};
-    for (int i = 0; i < 4; ++i) {
-        for (const HeadsSpan& x : ins)
-            if (outs[i].meets(x.bytes(1, rows, d, size))) return GFWA_ERR_OVERLAP;
-        if (outs[i].meets(gate)) return GFWA_ERR_OVERLAP;
-        for (int j = 0; j < i; ++j)
-            if (outs[i].meets(outs[j])) return GFWA_ERR_OVERLAP;
-    }
+    if (any_meet({outs[0], outs[1], outs[2], outs[3]},
+                 {ins[0].bytes(1, rows, d, size), ins[1].bytes(1, rows, d, size), ins[2].bytes(1, rows, d, size), gate, {wq, (size_t)d * 4}, {wk, (size_t)d * 4},
+                  {rot > 0 ? freq : nullptr, (size_t)rot * 4}, {start, ((size_t)B + 1) * 4}, {cached, (size_t)B * 4}, {table, (size_t)B * max_pages * 4}}))
+        return GFWA_ERR_OVERLAP;
     const HeadRotation how{wq, wk, eps, freq, rot, nullptr, (flags & GFWA_HEAD_NORM) != 0, (flags & GFWA_ROPE_PAIRED) != 0};
     const PagedCache cache{Kp, Vp, cp, table, pages, page, max_pages};
     return hip_status(append_paged(dt == GFWA_BF16, view(q), view(k), view(v), how, alpha, alpha_token, alpha_head, start, cached, Q, cache, rows,
@@ -445,8 +457,13 @@ int gfwa_decode_paged(gfwa_dtype_t dt, const void* q, const void* Kp, const void
     if (!aligned(q, 16) || !aligned(Kp, 16) || !aligned(Vp, 16) || !aligned(o, 16) || !aligned(cp, 4) || !aligned(table, 4) ||
         !aligned(pos, 4) || !aligned(L, 4))
         return GFWA_ERR_ALIGN;
-    if (!workspace || workspace_bytes < gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, w)) return GFWA_ERR_WORKSPACE;
+    const size_t scratch = gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, w);
+    if (!workspace || workspace_bytes < scratch) return GFWA_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return GFWA_ERR_ALIGN;
+    const size_t size = dt == GFWA_BF16 ? 2 : 4, row = (size_t)d * size, per_head = (size_t)pages * page, heads = (size_t)B * H;
+    if (any_meet({{o, heads * row}, {L, heads * 4}, {workspace, scratch}},
+                 {{q, heads * row}, {Kp, per_head * Hkv * row}, {Vp, per_head * Hkv * row}, {cp, per_head * H * 4}, {table, (size_t)B * max_pages * 4}, {pos, (size_t)B * 4}}))
+        return GFWA_ERR_OVERLAP;
     const PagedCache cache{const_cast<void*>(Kp), const_cast<void*>(Vp), const_cast<float*>(cp), table, pages, page, max_pages};
     return hip_status(decode_paged(dt == GFWA_BF16, q, cache, pos, o, L, (float*)workspace, B, H, Hkv, d, w, scale, stream));
 }
@@ -462,7 +479,7 @@ const char* gfwa_strerror(int code) {
             return "workspace missing or smaller than the matching gfwa_*_workspace_bytes() call asks for; for "
                    "gfwa_decode_static: the sizes need more than the library's 32 MiB of scratch";
         case GFWA_ERR_HIP: return g_hip_msg;
-        case GFWA_ERR_OVERLAP: return "an output overlaps an input, or its own rows overlap";
+        case GFWA_ERR_OVERLAP: return "an output overlaps an input, another output or the workspace, or its own rows overlap";
         default: return "unknown status code";
     }
 }

@@ -439,9 +439,10 @@ const at::Tensor& dense(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype
 const void* optional_input(PyObject* o, at::IntArrayRef shape, at::ScalarType dtype, const OneDevice& dev, const char* name) {
     return o == Py_None ? nullptr : dense(o, shape, dtype, dev, name).const_data_ptr();
 }
-int sizes_to_int(int64_t n, const char* what) {
-    if (n > 0x7fffffffLL) fail(PyExc_ValueError, std::string(what) + " is too large");
-    return (int)n;
+// sizes that are passed on as C ints
+void fits_int(at::IntArrayRef sizes) {
+    for (int64_t n : sizes)
+        if (n > 0x7fffffffLL) fail(PyExc_ValueError, "a size of " + std::to_string(n) + " is too large");
 }
 
 // A strided tensor of heads, [B,N,heads,d] (or [rows,heads,d]): anything whose last dimension is contiguous.
@@ -483,7 +484,8 @@ struct Rotation {
             if (f.dim() != 1) fail(PyExc_ValueError, "freq must be [rot / 2]");
             const int64_t half[1] = {f.size(0)};
             freq = (const double*)dense(a[3], half, at::kDouble, dev, "freq").const_data_ptr();
-            rot = sizes_to_int(2 * half[0], "freq");
+            fits_int({2 * half[0]});
+            rot = (int)(2 * half[0]);
         }
         const int norm = PyObject_IsTrue(a[4]), paired = PyObject_IsTrue(a[5]);
         if (norm < 0 || paired < 0) throw PyError{};
@@ -515,6 +517,7 @@ PyObject* qk_norm_rope(PyObject* const* a) {  // q, k, v, wq, wk, eps, freq, nor
     const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
     if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d]");
     const int64_t B = q.size(0), N = q.size(1), H = q.size(2), d = q.size(3), Hkv = kv_heads(H, k.size(2));
+    fits_int({B, N, H, d});
     const int dt = storage_type(q);
     const at::ScalarType st = q.scalar_type();
     const OneDevice dev(q);
@@ -562,6 +565,7 @@ PyObject* qk_norm_rope_backward(PyObject* const* a) {
     const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
     if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d]");
     const int64_t B = q.size(0), N = q.size(1), H = q.size(2), d = q.size(3), Hkv = kv_heads(H, k.size(2));
+    fits_int({B, N, H, d});
     const int dt = storage_type(q);
     const at::ScalarType st = q.scalar_type();
     const OneDevice dev(q);
@@ -630,9 +634,7 @@ struct Pages {
             cp = (float*)(write ? ct.data_ptr() : const_cast<void*>(ct.const_data_ptr()));
         }
         table = (const int*)dense(t, ts, at::kInt, dev, "table").const_data_ptr();
-        sizes_to_int(pages, "the number of pages");
-        sizes_to_int(page, "the page");
-        sizes_to_int(max_pages, "the table");
+        fits_int({pages, page, max_pages, B, H, Hkv, d});
     }
 };
 
@@ -653,6 +655,7 @@ PyObject* append_paged(PyObject* const* a) {
         H = al.size(1);
     }
     kv_heads(H, Hkv);
+    fits_int({rows});
     const int dt = storage_type(k);
     const at::ScalarType st = k.scalar_type();
     const OneDevice dev(k);
@@ -685,7 +688,7 @@ PyObject* append_paged(PyObject* const* a) {
     call([&] {
         return lib.append_paged(dt, hq.get(), hk.get(), hv.get(), how.wq, how.wk, how.eps, how.freq, how.rot, how.flags, alpha, alpha_token,
                                 alpha_head, (const int*)start, (const int*)before, cache.table, Q ? Q->ptr : nullptr, cache.Kp, cache.Vp, cache.cp,
-                                sizes_to_int(rows, "rows"), (int)B, (int)H, (int)Hkv, (int)d, (int)cache.pages, (int)cache.page, (int)cache.max_pages,
+                                (int)rows, (int)B, (int)H, (int)Hkv, (int)d, (int)cache.pages, (int)cache.page, (int)cache.max_pages,
                                 stream());
     });
     return none_or(Q ? &*Q : nullptr);

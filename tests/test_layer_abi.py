@@ -140,6 +140,21 @@ def test_decode_refuses(lib, status, kw):
     assert decode(lib, **kw) == status
 
 
+# what a call writes against what it reads besides the rows, and against its workspace
+@pytest.mark.parametrize("call,kw", [
+    (rope, dict(pos=P(0x2000000))), (rope, dict(pos=P(0x2000000 - 76))), (rope, dict(freq=P(0x3000000))), (rope, dict(freq=P(0x4000000 - 248))), (rope, dict(wq=P(0x4000000 + 16))),
+    (rope_bwd, dict(dwq=P(0x5000000))), (rope_bwd, dict(dwq=P(0x2000000))), (rope_bwd, dict(dwq=P(0x8000000))), (rope_bwd, dict(dwq=P(0x1000000))), (rope_bwd, dict(dwq=P(0x10000))),
+    (rope_bwd, dict(dwq=P(0x11000), ws=P(0x4000000))), (rope_bwd, dict(dwq=P(0x11000), ws=P(0x8000000))), (rope_bwd, dict(dq=heads(0x10000, 5120, 512, 64))),
+    (append, dict(start=P(0x3000000))), (append, dict(cached=P(0x2000000))), (append, dict(table=P(0x5000000 - 20))), (append, dict(freq=P(0x4000000))),
+    (decode, dict(o=P(0x900000 + 512), q=P(0x900000), L=P(0x800000))), (decode, dict(o=P(0x900000), L=P(0x900000 + 1020), ws=P(0xa00000))),
+    (decode, dict(o=P(0x900000), ws=P(0x900000 + 1008))), (decode, dict(o=P(0x900000), ws=P(0xa00000), pos=P(0xa00000))),
+    (decode, dict(o=P(0x900000), ws=P(0xa00000), table=P(0x900000))), (decode, dict(o=P(0x900000), ws=P(0xa00000), Kp=P(0x900000 - 16))),
+    (decode, dict(o=P(0x900000), ws=P(0xa00000), cp=P(0xa00000 + 64))),
+])
+def test_overlaps_are_refused(lib, call, kw):
+    assert call(lib, **kw) == -7
+
+
 def test_decode_workspace(lib):
     f = lib.gfwa_decode_paged_workspace_bytes
     assert f(2, 4, 2, 128, 32, 100, 1000) >= 2 * 4 * 130 * 4

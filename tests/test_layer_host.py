@@ -74,6 +74,11 @@ with FakeTensorMode():
     dec = g.gfwa_decode_paged
     qd, pos = new(3, 4, 64), i32(3)
     refused(ValueError, "divide", dec, new(3, 3, 64), Kp, Kp, cp, table, pos, 4, 0.1)
+    many = (1 << 32) + 3
+    refused(ValueError, "too large", dec, new(many, 4, 64), Kp, Kp, cp, i32(many, 2), i32(many), 4, 0.1)
+    refused(ValueError, "too large", app, kr, kr, Kp, Kp, i32(many + 1), i32(many), i32(many, 2))
+    refused(ValueError, "too large", app, kr[:1].expand(many, 2, 64), kr[:1].expand(many, 2, 64), Kp, Kp, start, cached, table)
+    refused(ValueError, "too large", rope, q[:1].expand(many, 9, 4, 64), k[:1].expand(many, 9, 2, 64))
     refused(TypeError, "cp", dec, qd, Kp, Kp, None, table, pos, 4, 0.1)
     refused(ValueError, "shape", dec, qd, Kp, Kp, cp, table, i32(4), 4, 0.1)
     refused(TypeError, "int32", dec, qd, Kp, Kp, cp, table, new(3, dtype=torch.int64), 4, 0.1)
