@@ -2,7 +2,8 @@
 // values to their pages, and the gate's prefix carried on, in one launch.
 //   * rows of queries, keys and values are held and worked on as in qk_norm_rope.hip; a row's sequence is looked up from the batch's
 //     offsets and its page from the table, once for all its heads;
-//   * the prefix is a scan along each sequence and goes to workgroups of its own, which the launch begins with.
+//   * the prefix is a scan along each sequence and goes to workgroups of its own, which the launch begins with (us, H 32, Hkv 8, d 128, one prompt of
+//     8192 tokens: a wave for each head 83, in segments 50, without gates 43; 16 prompts of up to 2048 tokens 101 either way).
 #include "gfwa_internal.h"
 #include "head_rows.h"
 
@@ -26,7 +27,7 @@ struct AppendArgs {
     float* cp;
     int rows, B, H, Hkv, pages, page, max_pages;
     int scan_blocks;   // workgroups of the prefix, in front
-    int scan_heads;    // heads that a wave of them takes: 8, or 1
+    int segments;      // pieces that a long sequence's prefix is cut into; 0: a wave for a whole sequence
     Shares shares;     // of tiles of 1024 / D rows
 };
 
@@ -81,98 +82,142 @@ __device__ __forceinline__ double lane_value(double x, int lane) {
     return __builtin_bit_cast(double, i32x2{__builtin_amdgcn_readlane(v[0], lane), __builtin_amdgcn_readlane(v[1], lane)});
 }
 
-constexpr int kShort = 8;       // new tokens, and heads, that a wave takes in one go
-constexpr int kScanGroups = 8;  // groups of 64 tokens of a pass over a long sequence
+constexpr int kScanHeads = 8;    // heads that are taken together
+constexpr int kScanGroups = 8;   // groups of 64 tokens whose gates are on their way together
+constexpr int kScanTokens = 64 * kScanGroups;
 
-// New tokens n0 .. n1 of sequence b, whose cache holds `before` tokens: c of one head, by one wave.  The gates and page ids of the next 512
-// tokens are on their way while these are added up.
-__device__ void prefix_long(const AppendArgs& a, int b, int h, int n0, int n1, long long before, double c) {
+// A sequence's new rows n0 .. n1, and how many tokens its cache holds.
+struct NewTokens {
+    int n0, n1;
+    long long before;
+    __device__ __forceinline__ NewTokens(const AppendArgs& a, int b) {
+        const int from = a.start[b], to = a.start[b + 1];
+        n0 = min(max(from, 0), a.rows);
+        n1 = min(max(to, n0), a.rows);
+        before = a.cached[b];
+    }
+};
+
+// The prefix that sequence b's cache ends with.
+__device__ __forceinline__ double cached_prefix(const AppendArgs& a, int b, long long before, int h) {
+    int row = 0;
+    const int id = page_of(a, b, before - 1, row);
+    return id >= 0 ? (double)a.cp[((size_t)id * a.H + h) * a.page + row] : 0.0;
+}
+
+// c of the new tokens `from` .. `to` of sequence b for heads h and h + 1, by one wave; c: their prefixes in front of `from`.
+__device__ void prefix_heads(const AppendArgs& a, int b, const NewTokens& s, int h, int from, int to, double (&c)[2]) {
     const int lane = threadIdx.x & 63;
-    const float* alpha = a.alpha + h * a.alpha_head;
-    float x[2][kScanGroups];
-    int id[2][kScanGroups];
-    auto issue = [&](int n, auto buf) __attribute__((always_inline)) {
+    const long long last = (long long)a.max_pages * a.page - 1;
+    for (int n = from; n < to; n += kScanTokens) {
+        float x[2][kScanGroups];
+        int id[kScanGroups], row[kScanGroups];
 #pragma unroll
-        for (int u = 0; u < kScanGroups; ++u) {
-            const int t = n + 64 * u + lane;
-            x[decltype(buf)::value][u] = t < n1 ? alpha[t * a.alpha_token] : 0.f;
-            int row;
-            id[decltype(buf)::value][u] = t < n1 ? page_of(a, b, before + (t - n0), row) : -1;
+        for (int u = 0; u < kScanGroups; ++u) {  // (no condition at a load: all are on their way before the first one is waited for)
+            const int t = min(n + 64 * u + lane, to - 1);
+            const long long p = s.before + (t - s.n0);
+            const int at = (int)max(0LL, min(p, last)), i = at / a.page;
+            row[u] = at - i * a.page;
+            id[u] = a.table[(size_t)b * a.max_pages + i];
+            x[0][u] = a.alpha[t * a.alpha_token + h * a.alpha_head];
+            x[1][u] = a.alpha[t * a.alpha_token + min(h + 1, a.H - 1) * a.alpha_head];
+            if (p != at) row[u] = -1;  // outside the table
         }
-    };
-    auto add = [&](int n, auto buf) __attribute__((always_inline)) {
-        constexpr int k = decltype(buf)::value;
 #pragma unroll
         for (int u = 0; u < kScanGroups; ++u) {
-            const double s = wave_scan((double)x[k][u]);
-            if (id[k][u] >= 0) {  // a position in the table: 32 bits
-                const int p = (int)(before + (n - n0)) + 64 * u + lane;
-                a.cp[((size_t)id[k][u] * a.H + h) * a.page + p % a.page] = (float)(c + s);
+            const bool mine = n + 64 * u + lane < to, there = mine && row[u] >= 0 && id[u] >= 0 && id[u] < a.pages;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const double sum = wave_scan(mine ? (double)x[k][u] : 0.0);
+                if (there && h + k < a.H) a.cp[((size_t)id[u] * a.H + h + k) * a.page + row[u]] = (float)(c[k] + sum);
+                c[k] += lane_value(sum, 63);
             }
-            c += lane_value(s, 63);
-        }
-    };
-    constexpr int kPass = 64 * kScanGroups;
-    const std::integral_constant<int, 0> first;
-    const std::integral_constant<int, 1> second;
-    issue(n0, first);
-    for (int n = n0; n < n1; n += 2 * kPass) {
-        if (n1 - n > kPass) issue(n + kPass, second);
-        add(n, first);
-        if (n1 - n > kPass) {
-            if (n1 - n > 2 * kPass) issue(n + 2 * kPass, first);
-            add(n + kPass, second);
         }
     }
 }
 
-// c of the new tokens of sequence b for `heads` (1 or 8) heads from h0 on, by one wave.  A few tokens and eight heads: a lane for each of both.
-__device__ void prefix_of(const AppendArgs& a, int b, int h0, int heads) {
+// c of all new tokens of sequence b for eight heads from h0 on, by one wave.  A few tokens: a lane for each head and token.
+__device__ void prefix_short(const AppendArgs& a, int b, int h0) {
     const int lane = threadIdx.x & 63;
-    const int from = a.start[b], to = a.start[b + 1];
-    const long long before = a.cached[b];
-    const int n0 = min(max(from, 0), a.rows), n1 = min(max(to, n0), a.rows);
-    if (n0 == n1) return;
-    int row = 0;
-    const int prev = page_of(a, b, before - 1, row);
-    auto cached_c = [&](int h) { return prev >= 0 ? (double)a.cp[((size_t)prev * a.H + h) * a.page + row] : 0.0; };
-    const int last = min(h0 + heads, a.H);
-    if (heads == kShort && n1 - n0 <= kShort) {
-        const int t = lane / kShort, h = h0 + lane % kShort;
-        const bool mine = n0 + t < n1 && h < last;
+    const NewTokens s(a, b);
+    if (s.n0 == s.n1) return;
+    if (s.n1 - s.n0 <= 64 / kScanHeads) {
+        const int t = lane / kScanHeads, h = h0 + lane % kScanHeads;
+        const bool mine = s.n0 + t < s.n1 && h < a.H;
         int at = 0;
-        const int id = mine ? page_of(a, b, before + t, at) : -1;
-        double c = mine ? a.alpha[(n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
-        if (n1 - n0 > 1) {
+        const int id = mine ? page_of(a, b, s.before + t, at) : -1;
+        double c = mine ? a.alpha[(s.n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
+        if (s.n1 - s.n0 > 1) {
 #pragma unroll
-            for (int off = kShort; off < 64; off *= 2) {
+            for (int off = kScanHeads; off < 64; off *= 2) {
                 const double x = __shfl_up(c, off, 64);
                 if (lane >= off) c += x;
             }
         }
         if (!mine) return;
-        c += cached_c(h);
+        c += cached_prefix(a, b, s.before, h);
         if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + at] = (float)c;
         return;
     }
-    for (int h = h0; h < last; ++h) prefix_long(a, b, h, n0, n1, before, cached_c(h));
+    for (int h = h0; h < min(h0 + kScanHeads, a.H); h += 2) {
+        double c[2] = {cached_prefix(a, b, s.before, h), cached_prefix(a, b, s.before, min(h + 1, a.H - 1))};
+        prefix_heads(a, b, s, h, s.n0, s.n1, c);
+    }
+}
+
+// c of a segment of the new tokens of sequence b for eight heads from h0 on, by a workgroup: the gates in front of it are added up by all its threads (a
+// line of them serves all eight heads), then every wave takes two heads.  Nothing waits for another workgroup; what that costs is that the gates
+// are read as often as there are segments behind them.
+__device__ void prefix_segment(const AppendArgs& a, int b, int h0, int segment) {
+    const NewTokens s(a, b);
+    const int n = s.n1 - s.n0, len = kScanTokens * ((n + kScanTokens * a.segments - 1) / (kScanTokens * a.segments));
+    if (segment * len >= n) return;  // the same for the whole workgroup
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, from = s.n0 + segment * len;
+    __shared__ double sums[kAppendWaves][kScanHeads];
+    double sum = 0.0;
+    const float* alpha = a.alpha + min(h0 + lane % kScanHeads, a.H - 1) * a.alpha_head;
+    constexpr int kStep = 64 * kAppendWaves / kScanHeads, kLoads = 32;
+    for (int t0 = s.n0 + (int)threadIdx.x / kScanHeads; t0 < from; t0 += kStep * kLoads) {
+        float x[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) x[u] = alpha[min(t0 + kStep * u, from - 1) * a.alpha_token];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) sum += t0 + kStep * u < from ? x[u] : 0.f;
+    }
+#pragma unroll
+    for (int off = kScanHeads; off < 64; off *= 2) sum += __shfl_xor(sum, off, 64);
+    if (lane < kScanHeads) sums[wv][lane] = sum;
+    __syncthreads();
+    static_assert(kScanHeads == 2 * kAppendWaves, "two heads to a wave");
+    const int h = h0 + 2 * wv;
+    if (h >= a.H) return;
+    double c[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        c[k] = cached_prefix(a, b, s.before, min(h + k, a.H - 1));
+#pragma unroll
+        for (int i = 0; i < kAppendWaves; ++i) c[k] += sums[i][2 * wv + k];
+    }
+    prefix_heads(a, b, s, h, from, min(from + len, s.n1), c);
 }
 
 template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
     if ((int)blockIdx.x < a.scan_blocks) {
-        // the heads of a sequence on one XCD: they read the same lines of alpha
-        const long long i = (long long)xcd_remap(blockIdx.x, a.scan_blocks) * kAppendWaves + (threadIdx.x >> 6);
-        const int units = (a.H + a.scan_heads - 1) / a.scan_heads;
-        if (i < (long long)a.B * units) prefix_of(a, (int)(i / units), (int)(i % units) * a.scan_heads, a.scan_heads);
+        const int block = xcd_remap(blockIdx.x, a.scan_blocks), units = (a.H + kScanHeads - 1) / kScanHeads;  // a sequence on one XCD: its heads share lines of alpha
+        if (a.segments > 0) {
+            const int i = block / units;
+            prefix_segment(a, i / a.segments, (block - i * units) * kScanHeads, i % a.segments);
+        } else {
+            const int i = block * kAppendWaves + (threadIdx.x >> 6);
+            if (i < a.B * units) prefix_short(a, i / units, i % units * kScanHeads);
+        }
         return;
     }
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
     const int all = (a.Q != nullptr ? a.H : 0) + 2 * a.Hkv, keys = all - 2 * a.Hkv, values = all - a.Hkv;  // numbers of the first key, the first value
-    Frequencies freq;
-    if (a.rot > 0) freq.load(l, a.freq);
     for (int item = (blockIdx.x - a.scan_blocks) * kAppendWaves + wv; item < a.shares.items; item += (gridDim.x - a.scan_blocks) * kAppendWaves) {
         int tile;
         const HeadRange range = a.shares.range(item, tile);
@@ -184,13 +229,16 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const A
         Angles angles;
         auto look_up = [&]() __attribute__((always_inline)) {
             if (b != -2) return;
+            Frequencies freq;  // here, not in front of the loop: that takes three waves a SIMD where four have room (7168 tokens 48 us, 39)
+            const bool turned = range.x0 < values && a.rot > 0;
+            if (turned) freq.load(l, a.freq);
             int first, before;
             b = n < a.rows ? sequence_of(a, (int)n, first, before) : -1;
             if (b >= 0) {
-                p = (long long)before + ((int)n - first);
-                if (before >= 0 && range.x1 > keys) id = page_of(a, b, p, row);
+                p = before + (n - first);
+                if (range.x1 > keys) id = page_of(a, b, p, row);
             }
-            if (range.x0 < values && a.rot > 0) angles.at(l, (int)p, freq);
+            if (turned) angles.at(l, (int)p, freq);
         };
         auto heads_of = [&](const HeadsView& in, const float* weight, void* out, int first, int count, auto kind) __attribute__((always_inline)) {
             constexpr HeadKind K = decltype(kind)::value;
@@ -251,11 +299,15 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.page = cache.page;
     a.max_pages = cache.max_pages;
     constexpr int kThreads = 64 * kAppendWaves;
-    // a wave of the prefix takes one head where sequences bring many tokens (more than 16 on average: those with few leave
-    // its lanes idle, those with many are bound by it), eight where they bring few
-    a.scan_heads = rows > 16LL * B ? 1 : kShort;
-    const long long scans = (long long)B * ((H + a.scan_heads - 1) / a.scan_heads);
-    a.scan_blocks = alpha != nullptr ? (int)((scans + kAppendWaves - 1) / kAppendWaves) : 0;
+    // The prefix.  In a decoding step (no more rows than sequences) a wave takes eight heads of a sequence, however many tokens that has; otherwise a
+    // workgroup does, for a segment of it: of 512 tokens, or as many as keep the segments to 64 and all sequences' to about 4096 workgroups.
+    const int units = (H + kScanHeads - 1) / kScanHeads, sequences = B * units;
+    if (alpha != nullptr && rows > B) {
+        const int most = sequences < 4096 ? 4096 / sequences : 1, want = (rows + kScanTokens - 1) / kScanTokens;
+        a.segments = want < most ? want : most;
+        if (a.segments > 64) a.segments = 64;
+    }
+    a.scan_blocks = alpha == nullptr ? 0 : a.segments > 0 ? sequences * a.segments : (sequences + kAppendWaves - 1) / kAppendWaves;
     const int side = d == 128 ? kSide<128> : kSide<64>;
     a.shares = Shares((int)(((long long)rows * side + 1024 / d - 1) / (1024 / d)), (Q != nullptr ? H : 0) + 2 * Hkv, side);
     long long blocks = ((long long)a.shares.items + kAppendWaves - 1) / kAppendWaves;

@@ -13,7 +13,8 @@ namespace {
 constexpr int kUnit = 16;       // positions of a unit; pages are multiples of it
 constexpr float kNone = -3.0e38f;  // reference of no key yet: finite, so that differences of references are numbers, and below every score that counts
 
-constexpr int kFewChunks = 16;
+constexpr int kFewChunks = 16;  // chunks whose records all are written and merged by one group of threads (two rounds of loads)
+constexpr long long kOnceWindows = 24 << 20;  // windows of more than this in all are not met in the L2s (32 MiB) again
 
 // Partial result of one (query head, chunk): D output columns (not yet divided by the sum), the exponent they are scaled
 // by (log2 domain) and the sum.
@@ -234,11 +235,12 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // the next tile are on their way while a tile is worked on.  A head's weights are taken against a reference that is raised, and sums rescaled,
 // only when a score exceeds it by 2^16.
 // (The page numbers of the tile after that could be asked for ahead too: eight more registers, which bf16 at d = 128 does not have beside three waves a
-// SIMD; whole sequences, H 32, Hkv 8, 4 of up to 8192 22.3 us with and 19.5 without, 16
-// 68.3 and 65.4, 128 windows of 512 keys 49.3 and 51.7.  Two tiles ahead: 22.1, 68.1 and 47.6, in fp32 past the registers.)
+// SIMD; whole sequences, H 32, Hkv 8, 4 of up to 8192 22.3 us with and 19.5 without, 16 of them 68.3 and 65.4, 128 windows of 512 keys 49.3 and 51.7.
+// Two tiles ahead: 22.1, 68.1 and 47.6, in fp32 past the registers.)
 // ONCE: V is loaded past the caches.  No other workgroup reads it, and a window that the L2s do not hold is read faster (us, bf16, H 32, Hkv 8, d 128,
-// w 1024: 64 sequences 49.4 -> 46.0, 32 26.1 -> 22.8; H 32, Hkv 4, d 64, whole sequences of up to 16384 40.7 -> 33.8), one that they do hold more
-// slowly (2 sequences of H 16, d 64, w 512, 4 MB, 6.7 -> 7.2).  K's lines are asked for by two loads each: past the caches 47.6 for the first.
+// w 1024: 64 sequences 48.7 -> 46.3, 32 26.4 -> 22.5, 12 that no cache holds 16.9 -> 16.2; fp32, 64 sequences 91 -> 85; H 32, Hkv 4, d 64, whole
+// sequences of up to 16384 40.6 -> 35), one that they do hold more slowly (2 sequences of H 16, d 64, w 512, 4 MB, 6.7 -> 7.2).  K's lines are asked for
+// by two loads each: past the caches the 64 sequences take 47.6.
 template <typename T, int D, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArgs a) {
     typedef Tile<T, D> Tl;
@@ -494,11 +496,11 @@ struct Plan {
         waves = 4;
         // Measured (us, four and eight waves, graphs of 21 steps; H 32, Hkv 8, d 128 unless named):
         //   * a window shorter than the table is about as long for every sequence.  Where one chunk each gives every compute unit two
-        //     workgroups of four waves that is best (64 sequences, w 1024: one chunk 49, two 54); with half of that, one of eight
-        //     waves (32 sequences: 26; two chunks of four waves 29); with fewer, chunks for two workgroups (8: 11.8, for one 13.0).
+        //     workgroups of four waves that is best (64 sequences, w 1024: one chunk 46, two 53); with half of that, one of eight
+        //     waves (32 sequences: 22.5; two chunks of four waves 25.4); with fewer, chunks for two workgroups (8: 12.1, for one 13.4).
         //   * whole sequences are of any length: chunks of two tiles a wave, or as many as make 4096 workgroups, level that (16 of up
-        //     to 8192: 70; 512 workgroups 79; H 32, Hkv 4, d 64, up to 16384: 41 and 53).
-        //   * a window of three tiles a wave is not worth the merge (300 keys of one sequence: 4.4, in three chunks 6.3).
+        //     to 8192: 66; 512 workgroups 81; H 32, Hkv 4, d 64, up to 16384: 35 and 47).
+        //   * a window of three tiles a wave is not worth the merge (300 keys of one sequence: 4.6, in three chunks 6.1).
         const bool even = w < (long long)max_pages * page;
         long long S = 1;
         least = waves;
@@ -535,7 +537,7 @@ static hipError_t launch(const PagedArgs& given, int B, hipStream_t s) {
         ProfScope prof(kKernDecodePaged, s);
         auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.items * a.splits)), dim3(threads), 0, s, a); };
         const long long keys = (long long)a.max_pages * a.page, span = a.w < keys ? a.w : keys;
-        const bool once = plan.items == (long long)B * a.Hkv && plan.items * span * D * 2 * (long long)sizeof(T) > kOnceBytes;
+        const bool once = plan.items == (long long)B * a.Hkv && plan.items * span * D * 2 * (long long)sizeof(T) > kOnceWindows;
         if (plan.waves == 8) once ? go(decode_paged_kernel<T, D, 8, true>, 512) : go(decode_paged_kernel<T, D, 8, false>, 512);
         else once ? go(decode_paged_kernel<T, D, 4, true>, 256) : go(decode_paged_kernel<T, D, 4, false>, 256);
     }

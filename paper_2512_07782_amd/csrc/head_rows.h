@@ -196,11 +196,12 @@ struct LaneVector {
 };
 
 // The two units of a lane's row.
-// ONCE: loaded past the caches, where a load takes whole lines (bf16, D = 128).  Inputs that the L2s do not hold are read faster (us, H 32, Hkv 8,
-// N 16384: forward 86 -> 74, backward 127 -> 107), those that they may still hold from their making as before.
+// ONCE: loaded past the caches, where a load takes whole lines (bf16, D = 128).  Large inputs are read faster (us, H 32, Hkv 8, N 16384: forward 84 -> 81,
+// backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8), those that are small enough to be held from their
+// making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
 template <typename T, int D>
 constexpr bool kWholeLines = sizeof(T) == 2 && D == 128;
-constexpr long long kOnceBytes = 24 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
+constexpr long long kOnceBytes = 40 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
 template <typename T, int D, bool ONCE = false>
 struct LaneRow {
     Unit8<T> a, b;
@@ -208,9 +209,9 @@ struct LaneRow {
         a.template load<ONCE && kWholeLines<T, D>>(row + l.a);
         b.template load<ONCE && kWholeLines<T, D>>(row + l.b);
     }
-    // PAST: stored past the caches, for what nothing reads soon.  (Stored like that, the results of norm and rotation cost less themselves, us, H 32,
-    // Hkv 8, N 16384: forward 88 -> 84, backward 129 -> 121, and the kernel that reads them right after more: rope and attention in a row 226
-    // -> 233, at B 4, H 16, Hkv 4, N 4096, d 64 73 -> 78, the backward and a matrix product with its result 407 -> 412.)
+    // PAST: stored past the caches, for what nothing reads soon.  (The cache's new rows: 16 prompts 109 -> 103 us.  The results of norm and rotation would
+    // cost less themselves, us, H 32, Hkv 8, N 16384: forward 85 -> 83, backward 120 -> 117, and the kernel that reads them right after more: rope
+    // and attention in a row 226 -> 233, at B 4, H 16, Hkv 4, N 4096, d 64 73 -> 78, the backward and a matrix product with its result 407 -> 412.)
     template <bool PAST = false>
     __device__ __forceinline__ void store(T* row, const LaneOfRow<D>& l) const {
         a.template store<PAST>(row + l.a);
@@ -237,9 +238,9 @@ struct LaneRow {
 };
 
 // Heads of a token that a wave takes side by side: what it reads of a token-major tensor comes in runs of kSide rows, what it writes of a head-major one in
-// runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16384, d 128 89 / 83 / 85 / 88, of N 16640 99 / 96 /
-// 89 / -, backward of N 16640 167 / 147 / 125 / -, append of 16 prompts 119 / 108 / 106 / 125; rows of 4 lanes: backward of B 4, H 16, Hkv 4, N 4096,
-// d 64 39.5 / 35.5 / 39.8 / 51.)
+// runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16640, d 128 96 / 97 / 90 / 84, backward 151 / 142 / 125 /
+// 119, of N 16384 133 / 125 / 120 / 123, of H 16, Hkv 4, N 4100 21 / 21 / 22 / 30, append of 16 prompts 114 / 108 / 101 / 105; rows of 4 lanes, B 4, H 16, Hkv 4,
+// N 4096, d 64: forward 25.4 / 23.9 / 26.1 / 27.7, backward 38.7 / 37.8 / 38.4 / 46.)
 template <int D>
 constexpr int kSide = D == 128 ? 4 : 2;
 

@@ -3,8 +3,8 @@
 // the attention's head-major layout (or back).
 //   * a row of D elements is held by D / 16 lanes (head_rows.h), so that the norm's sum takes two or three DPP exchanges, the rotation
 //     none, and every access is whole 16-byte pieces;
-//   * a wave takes two (D = 128) or eight (D = 64) consecutive tokens, four or two heads of each at a time, and walks over a range of heads: a token's
-//     angles are formed once for all of them, and both layouts are met in runs (kSide);
+//   * a wave takes two (D = 128) or eight (D = 64) consecutive tokens, four or two heads of each at a time (kSide; kManySide), and walks over a range of
+//     heads: a token's angles are formed once for all of them, and both layouts are met in runs;
 //   * the weights' gradients are summed in registers over all rows of a wave, over the waves through LDS and over the workgroups by
 //     a second small launch, in an order that does not change from run to run.
 #include "gfwa_internal.h"
@@ -46,9 +46,9 @@ struct LaneToken {
     __device__ __forceinline__ long long dense(int heads, int N) const { return (long long)b * heads * N + n; }  // row of the first head
 };
 
-template <typename T, int D, bool ONCE>
+template <typename T, int D, bool ONCE, int HG>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const RopeArgs a) {
-    constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
+    constexpr int LPR = D / 16, RPW = 64 / LPR / HG;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
     Frequencies freq;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
 #pragma unroll
     for (int i = 0; i < 32; ++i) sums[wv][i >> 4][i & 15][lane] = 0.f;
     struct Rows {
-        LaneRow<T, D, ONCE> g;  // (the inputs past the caches too: 127 us against 123 at H 32, Hkv 8, N 16384, d 128)
+        LaneRow<T, D, ONCE> g;  // (the inputs past the caches too: 123 us against 120 at H 32, Hkv 8, N 16384, d 128)
         LaneRow<T, D> x;
     };
     Frequencies freq;
@@ -221,12 +221,17 @@ __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __re
 }
 
 // Workgroups that leave sums of the weights' gradients: three waves a SIMD are there at a time (bf16), and what fits in them goes at once; more goes through
-// two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 120 / 123, B 4, H 16, N 8192 208 /
-// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 27 / 23 / 23).
+// two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 122 / 124, B 4, H 16, N 8192 207 /
+// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 27 / 22 / 22).
 constexpr int kMostSums = 768, kManySums = 512;
 
-long long share_out(RopeArgs& a, int D) {
-    const int side = D == 128 ? kSide<128> : kSide<64>;
+// Forward: eight heads side by side where the queries and the keys have a multiple of eight and more than 128 MiB are read; what a wave reads is then one
+// token's (us, kSide / eight: H 32, Hkv 8, d 128, N 32768 174 / 155, 16384 88 / 81, 12000 65 / 62, 8192 41.5 / 42.2, 4096 22.8 / 22.7, 1024 10.2 / 10.9;
+// B 8, H 16, N 8192, d 64 164 / 157; fp32, B 2, H 16, N 4400 100 / 93).
+constexpr int kManySide = 8;
+constexpr long long kManyBytes = 128 << 20;
+
+long long share_out(RopeArgs& a, int D, int side) {
     a.shares = Shares((int)(((long long)a.tokens * side + 1024 / D - 1) / (1024 / D)), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
     const long long blocks = ((long long)a.shares.items + kRopeWaves - 1) / kRopeWaves;
     if (a.part != nullptr) return blocks <= kMostSums ? blocks : kManySums;
@@ -263,16 +268,21 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.q = q;
     a.k = k;
     a.v = v;
-    const long long blocks = share_out(a, d);
+    const long long bytes = (long long)a.tokens * (H + 2LL * Hkv) * d * (bf16 ? 2 : 4);
+    const bool many = H % kManySide == 0 && Hkv % kManySide == 0 && bytes > kManyBytes, once = bytes > kOnceBytes;
+    const long long blocks = share_out(a, d, many ? kManySide : d == 128 ? kSide<128> : kSide<64>);
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
-    if (bf16) {
-        const bool once = (long long)a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
-        if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_kernel<bf16_t, 128, false>);
-        else launch(qk_norm_rope_kernel<bf16_t, 64, false>);
-    } else {
-        d == 128 ? launch(qk_norm_rope_kernel<float, 128, false>) : launch(qk_norm_rope_kernel<float, 64, false>);
-    }
+    auto of_side = [&](auto side) {
+        constexpr int HG128 = decltype(side)::value ? kManySide : kSide<128>, HG64 = decltype(side)::value ? kManySide : kSide<64>;
+        if (bf16) {
+            if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true, HG128>) : launch(qk_norm_rope_kernel<bf16_t, 128, decltype(side)::value, HG128>);  // (eight: always ONCE)
+            else launch(qk_norm_rope_kernel<bf16_t, 64, false, HG64>);
+        } else {
+            d == 128 ? launch(qk_norm_rope_kernel<float, 128, false, HG128>) : launch(qk_norm_rope_kernel<float, 64, false, HG64>);
+        }
+    };
+    many ? of_side(std::true_type{}) : of_side(std::false_type{});
     return hipGetLastError();
 }
 
@@ -286,7 +296,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.x_q = q;
     a.x_k = k;
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
-    const long long blocks = share_out(a, d);
+    const long long blocks = share_out(a, d, d == 128 ? kSide<128> : kSide<64>);
     {
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };

@@ -130,6 +130,25 @@ def test_norm_and_rotation(g, B, H, Hkv, N, d, rot, paired, norm, kind, pos_kind
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,N,d", [(8, 8, 22223, 128), (16, 8, 33335, 64)])
+def test_large_inputs_as_small_ones(g, H, Hkv, N, d, dtype):
+    """More than 128 MiB, which a wave walks through in another order: the bits of calls for a part of the tokens."""
+    gen = torch.Generator(device=DEV).manual_seed(N)
+    x = torch.randn(1, N, H + 2 * Hkv, d, device=DEV, generator=gen).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q, k, v = x[:, :, :H], x[:, :, H:H + Hkv], x[:, :, H + Hkv:]
+    assert x.numel() * x.element_size() > 128 << 20
+    w = 1 + 0.3 * torch.randn(2, d, device=DEV, generator=gen)
+    f = dev64(freq_of(d))
+    for kw in (dict(freq=f, wq=w[0], wk=w[1]), dict(freq=f, norm=False, paired=True)):
+        whole = g.gfwa_qk_norm_rope(q, k, v, **kw)
+        for i in range(0, N, 5000):
+            at = slice(i, min(i + 5000, N))
+            pos = torch.arange(at.start, at.stop, dtype=torch.int32, device=DEV)[None]
+            part = g.gfwa_qk_norm_rope(q[:, at], k[:, at], v[:, at], pos=pos, **kw)
+            assert all(torch.equal(a[:, :, at], b) for a, b in zip(whole, part)), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,H,Hkv,N,d,rot,paired,norm,kind,pos_kind", ROPE)
 def test_norm_and_rotation_backward(g, B, H, Hkv, N, d, rot, paired, norm, kind, pos_kind, dtype):
     print("rope bwd", B, H, Hkv, N, d, rot, paired, norm, kind, pos_kind, dtype, flush=True)
@@ -259,6 +278,8 @@ APPEND = [
     ([(0, 1500), (2, 3)], 16, 2, 64, 128, 64, False, True, 0, 0, ()),
     ([(0, 0), (0, 0), (9, 2), (0, 0)], 3, 3, 128, 16, 128, True, True, 4, 4, ()),
     ([(0, 5)] * 9 + [(0, 3000)] + [(1, 1)] * 5, 2, 2, 64, 256, 64, False, True, 0, 7, ()),
+    ([(40, 2600), (0, 1), (7, 511), (0, 0), (5, 513)], 9, 3, 64, 64, 0, False, False, 2, 3, ((0, 20),)),  # prefixes in segments
+    ([(3, 40000)], 1, 1, 64, 512, 16, False, True, 0, 0, ()), ([(5, 0)] * 69 + [(9, 70)], 5, 5, 64, 16, 0, False, False, 0, 0, ()),
 ]
 
 
