@@ -770,3 +770,83 @@ def test_decode_short_sequences_in_a_long_table(g, B, Hkv, G, d, dtype):
     n = min(lens[0], 38)
     wide[0, -3:] = np.resize(table[0], 3)
     decode_check(g, dtype, q, tq, K1, V1, cp, tK, tV, tc, wide, [65536 - 48 + n - 1] + pos[1:], n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_training_step_and_prompt(g, dtype):
+    """Norm and rotation, its derivative and the append of prompts (prefixes in segments) as one graph, replayed on other contents of the same tensors:
+    the bits of eager calls each time."""
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    H, Hkv, N, d, page = 8, 2, 1300, 64, 32
+    new = lambda *s: torch.empty(s, device=DEV, dtype=dt)
+    x, dx, wt = new(1, N, H + 2 * Hkv, d), new(1, N, H + 2 * Hkv, d), torch.empty(2, d, device=DEV)
+    grads = [new(1, h, N, d) for h in (H, Hkv, Hkv)]
+    outs, Qn = [new(1, h, N, d) for h in (H, Hkv, Hkv)], new(N, H, d)
+    dw = torch.empty(2, d, device=DEV)
+    alpha = torch.empty(N, H, device=DEV)
+    start, cached = (torch.tensor(v, dtype=torch.int32, device=DEV) for v in ([0, 1100, N], [5, 40]))
+    table = torch.randperm(2 * 36, device=DEV, generator=gen).view(2, 36).int()
+    cache = [torch.zeros(72, Hkv, page, d, device=DEV, dtype=dt), torch.zeros(72, Hkv, page, d, device=DEV, dtype=dt), torch.zeros(72, H, page, device=DEV)]
+    ws = torch.empty(g.gfwa_qk_norm_rope_backward_workspace_bytes(1, H, Hkv, N, d), dtype=torch.uint8, device=DEV)
+    f = dev64(freq_of(d))
+    parts = lambda t: (t[..., :H, :], t[..., H:H + Hkv, :], t[..., H + Hkv:, :])
+
+    def step():
+        q, k, v = parts(x)
+        dq, dk, dv = parts(dx)
+        g.gfwa_qk_norm_rope(q, k, v, wt[0], wt[1], freq=f, Q=outs[0], K=outs[1], V=outs[2])
+        g.gfwa_qk_norm_rope_backward(q, k, *grads, wt[0], wt[1], freq=f, dq=dq, dk=dk, dv=dv, dwq=dw[0], dwk=dw[1], workspace=ws)
+        g.gfwa_append_paged(k[0], v[0], cache[0], cache[1], start, cached, table, q=q[0], wq=wt[0], wk=wt[1], freq=f, alpha=alpha, cp=cache[2], Q=Qn)
+
+    written = [dx, dw, Qn, *outs, *cache]
+
+    def refill(i):
+        gen.manual_seed(100 + i)
+        for t in [x, wt, *grads]:
+            t.copy_(torch.randn(t.shape, device=DEV, generator=gen))
+        alpha.copy_(torch.rand(alpha.shape, device=DEV, generator=gen))
+        for t in cache:
+            t.fill_(0.25)
+        for t in written[:-3]:
+            t.fill_(7.0)
+
+    refill(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in range(4):
+        refill(i)
+        step()
+        torch.cuda.synchronize()
+        eager = [t.clone() for t in written]
+        refill(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, written)), i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sequences_that_share_pages(g, dtype):
+    """Three sequences on the same first pages, each appending to a page of its own, one of them twice in the batch of the step."""
+    H, Hkv, d, page = 8, 2, 64, 16
+    rng, table, Kp, Vp, cp = paged_case(21, [(48, 2), (48, 2), (48, 2)], H, Hkv, d, page, dtype)
+    table[1:, :3] = table[0, :3]
+    start, cached = np.array([0, 2, 4, 6], dtype=np.int32), np.full(3, 48, dtype=np.int32)
+    q, k, v = (store(rng.standard_normal((6, h, d)), dtype) for h in (H, Hkv, Hkv))
+    alpha = (rng.random((6, H)) * 0.3).astype(np.float32)
+    (K1, tK), (V1, tV), tc = store(Kp, dtype), store(Vp, dtype), gpu(cp)
+    g.gfwa_append_paged(k[1], v[1], tK, tV, gpu(start), gpu(cached), gpu(table), norm=False, alpha=gpu(alpha), cp=tc)
+    _, Kr, Vr, cr = ol.append_paged(q[0], k[0], v[0], None, None, EPS, False, None, False, alpha, start, cached, table, q[0], K1, V1, cp)
+    assert np.array_equal(host(tK), Kr, equal_nan=True) and np.array_equal(host(tV), Vr, equal_nan=True)  # no arithmetic
+    got = host(tc)
+    fin = ~np.isnan(cr)
+    assert np.array_equal(~np.isnan(got), fin) and (np.abs(got[fin] - cr[fin]) <= U * np.abs(cr[fin])).all()
+    rows = [0, 1, 2, 1]
+    qs, tq = store(rng.standard_normal((4, H, d)), dtype)
+    decode_check(g, dtype, qs, tq, Kr, Vr, got.astype(np.float32), tK, tV, tc, table[rows], [49, 49, 49, 48], 30)
