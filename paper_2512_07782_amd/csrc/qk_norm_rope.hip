@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
 template <typename T, int D, bool ONCE>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const RopeArgs a) {
     constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
-    __shared__ float sums[kRopeWaves][2][16][64];  // of each lane's elements, for the queries' and the keys' weights
+    __shared__ float sums[kRopeWaves][2][16][64 + LPR];  // of each lane's elements, for the queries' and the keys' weights (LPR: rows do not meet in a bank)
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
 #pragma unroll
