@@ -8,8 +8,8 @@ Tolerances.  half = eps / 2 of the storage type (2^-8 bf16, 2^-24 fp32): one rou
   dw: products off by 32 u, sums of at most 16 + 3 + 4 + 64 + 32 terms in a chain (rows of a lane: the tests' sizes give each lane at most 16): 160 u of
   the sum of magnitudes.
   c: fp64 sums rounded once: u.
-  decode: scores from n = d products in fp32, d + 8 units of scale sum|q||k| and 8 units of |S|: E; weights off by 2 E + 8 u and, in bf16, rounded
-  to bf16 on their way into the second product (half); sums of n keys off by at most n units; the quotient is rounded to the storage type.
+  decode: scores from n = d products in fp32, d + 8 units of scale sum|q||k| and 8 units of |S|: E; weights off by 2 E + 8 u and, in bf16, taken
+  as two bf16 numbers into the second product (2^-16 of each, twice that for the sums of their parts); sums of n keys off by at most n units; the quotient is rounded to the storage type.
 """
 import numpy as np
 import pytest
@@ -379,7 +379,7 @@ def decode_check(g, dtype, q, tq, Kp, Vp, cp, tK, tV, tc, table, pos, w, **kw):
     E = ((d + 8) * dots + 8 * top) * U
     n = count[:, None]
     rel = 2 * E + (n + 16) * U
-    tol = HALF[dtype] * np.abs(o_ref) + (rel + (2 * HALF["bf16"] if dtype == "bf16" else 0))[..., None] * absv
+    tol = HALF[dtype] * np.abs(o_ref) + (rel + (2.0 ** -15 if dtype == "bf16" else 0))[..., None] * absv
     with np.errstate(invalid="ignore"):  # empty rows: minus infinity on both sides
         err, lerr = np.abs(host(o) - o_ref), host(L) - L_ref
     empty = np.isinf(L_ref)
