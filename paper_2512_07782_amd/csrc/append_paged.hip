@@ -105,29 +105,31 @@ __device__ __forceinline__ double cached_prefix(const AppendArgs& a, int b, long
     return id >= 0 ? (double)a.cp[((size_t)id * a.H + h) * a.page + row] : 0.0;
 }
 
-// c of the new tokens `from` .. `to` of sequence b for heads h and h + 1, by one wave; c: their prefixes in front of `from`.
-__device__ void prefix_heads(const AppendArgs& a, int b, const NewTokens& s, int h, int from, int to, double (&c)[2]) {
+// c of the new tokens `from` .. `to` of sequence b for the heads h .. h + HEADS - 1, by one wave, 64 GROUPS tokens at a time; c: their prefixes in front
+// of `from`.
+template <int HEADS, int GROUPS>
+__device__ __forceinline__ void prefix_heads(const AppendArgs& a, int b, const NewTokens& s, int h, int from, int to, double (&c)[HEADS]) {
     const int lane = threadIdx.x & 63;
     const long long last = (long long)a.max_pages * a.page - 1;
-    for (int n = from; n < to; n += kScanTokens) {
-        float x[2][kScanGroups];
-        int id[kScanGroups], row[kScanGroups];
+    for (int n = from; n < to; n += 64 * GROUPS) {
+        float x[HEADS][GROUPS];
+        int id[GROUPS], row[GROUPS];
 #pragma unroll
-        for (int u = 0; u < kScanGroups; ++u) {  // (no condition at a load: all are on their way before the first one is waited for)
+        for (int u = 0; u < GROUPS; ++u) {  // (no condition at a load: all are on their way before the first one is waited for)
             const int t = min(n + 64 * u + lane, to - 1);
             const long long p = s.before + (t - s.n0);
             const int at = (int)max(0LL, min(p, last)), i = at / a.page;
             row[u] = at - i * a.page;
             id[u] = a.table[(size_t)b * a.max_pages + i];
-            x[0][u] = a.alpha[t * a.alpha_token + h * a.alpha_head];
-            x[1][u] = a.alpha[t * a.alpha_token + min(h + 1, a.H - 1) * a.alpha_head];
+#pragma unroll
+            for (int k = 0; k < HEADS; ++k) x[k][u] = a.alpha[t * a.alpha_token + min(h + k, a.H - 1) * a.alpha_head];
             if (p != at) row[u] = -1;  // outside the table
         }
 #pragma unroll
-        for (int u = 0; u < kScanGroups; ++u) {
+        for (int u = 0; u < GROUPS; ++u) {
             const bool mine = n + 64 * u + lane < to, there = mine && row[u] >= 0 && id[u] >= 0 && id[u] < a.pages;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < HEADS; ++k) {
                 const double sum = wave_scan(mine ? (double)x[k][u] : 0.0);
                 if (there && h + k < a.H) a.cp[((size_t)id[u] * a.H + h + k) * a.page + row[u]] = (float)(c[k] + sum);
                 c[k] += lane_value(sum, 63);
@@ -136,33 +138,34 @@ __device__ void prefix_heads(const AppendArgs& a, int b, const NewTokens& s, int
     }
 }
 
-// c of all new tokens of sequence b for eight heads from h0 on, by one wave.  A few tokens: a lane for each head and token.
-__device__ void prefix_short(const AppendArgs& a, int b, int h0) {
-    const int lane = threadIdx.x & 63;
-    const NewTokens s(a, b);
-    if (s.n0 == s.n1) return;
-    if (s.n1 - s.n0 <= 64 / kScanHeads) {
-        const int t = lane / kScanHeads, h = h0 + lane % kScanHeads;
-        const bool mine = s.n0 + t < s.n1 && h < a.H;
-        int at = 0;
-        const int id = mine ? page_of(a, b, s.before + t, at) : -1;
-        double c = mine ? a.alpha[(s.n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
-        if (s.n1 - s.n0 > 1) {
+// c of at most eight new tokens of sequence b for eight heads from h0 on, by one wave: a lane for each head and token.
+constexpr int kFewTokens = 64 / kScanHeads;
+__device__ void prefix_few(const AppendArgs& a, int b, const NewTokens& s, int h0) {
+    const int lane = threadIdx.x & 63, t = lane / kScanHeads, h = h0 + lane % kScanHeads;
+    const bool mine = s.n0 + t < s.n1 && h < a.H;
+    int at = 0;
+    const int id = mine ? page_of(a, b, s.before + t, at) : -1;
+    double c = mine ? a.alpha[(s.n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
+    if (s.n1 - s.n0 > 1) {
 #pragma unroll
-            for (int off = kScanHeads; off < 64; off *= 2) {
-                const double x = __shfl_up(c, off, 64);
-                if (lane >= off) c += x;
-            }
+        for (int off = kScanHeads; off < 64; off *= 2) {
+            const double x = __shfl_up(c, off, 64);
+            if (lane >= off) c += x;
         }
-        if (!mine) return;
-        c += cached_prefix(a, b, s.before, h);
-        if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + at] = (float)c;
-        return;
     }
-    for (int h = h0; h < min(h0 + kScanHeads, a.H); h += 2) {
-        double c[2] = {cached_prefix(a, b, s.before, h), cached_prefix(a, b, s.before, min(h + 1, a.H - 1))};
-        prefix_heads(a, b, s, h, s.n0, s.n1, c);
-    }
+    if (!mine) return;
+    c += cached_prefix(a, b, s.before, h);
+    if (id >= 0) a.cp[((size_t)id * a.H + h) * a.page + at] = (float)c;
+}
+
+// c of all new tokens of sequence b for eight heads from h0 on, by one wave.
+__device__ void prefix_short(const AppendArgs& a, int b, int h0) {
+    const NewTokens s(a, b);
+    if (s.n1 - s.n0 <= kFewTokens) return prefix_few(a, b, s, h0);
+    double c[kScanHeads];
+#pragma unroll
+    for (int k = 0; k < kScanHeads; ++k) c[k] = cached_prefix(a, b, s.before, min(h0 + k, a.H - 1));
+    prefix_heads<kScanHeads, 2>(a, b, s, h0, s.n0, s.n1, c);
 }
 
 // c of a segment of the new tokens of sequence b for eight heads from h0 on, by a workgroup: the gates in front of it are added up by all its threads (a
@@ -172,6 +175,10 @@ __device__ void prefix_segment(const AppendArgs& a, int b, int h0, int segment) 
     const NewTokens s(a, b);
     const int n = s.n1 - s.n0, len = kScanTokens * ((n + kScanTokens * a.segments - 1) / (kScanTokens * a.segments));
     if (segment * len >= n) return;  // the same for the whole workgroup
+    if (n <= kFewTokens) {
+        if (threadIdx.x < 64) prefix_few(a, b, s, h0);
+        return;
+    }
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, from = s.n0 + segment * len;
     __shared__ double sums[kAppendWaves][kScanHeads];
     double sum = 0.0;
@@ -198,7 +205,7 @@ __device__ void prefix_segment(const AppendArgs& a, int b, int h0, int segment) 
 #pragma unroll
         for (int i = 0; i < kAppendWaves; ++i) c[k] += sums[i][2 * wv + k];
     }
-    prefix_heads(a, b, s, h, from, min(from + len, s.n1), c);
+    prefix_heads<2, kScanGroups>(a, b, s, h, from, min(from + len, s.n1), c);
 }
 
 template <typename T, int D, bool ONCE>
@@ -299,11 +306,13 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.page = cache.page;
     a.max_pages = cache.max_pages;
     constexpr int kThreads = 64 * kAppendWaves;
-    // The prefix.  In a decoding step (no more rows than sequences) a wave takes eight heads of a sequence, however many tokens that has; otherwise a
-    // workgroup does, for a segment of it: of 512 tokens, or as many as keep the segments to 64 and all sequences' to about 4096 workgroups.
+    // The prefix.  Where sequences bring two tokens or fewer on average a wave takes eight heads of a sequence, however many tokens that has; otherwise a
+    // workgroup does, for a segment of it: of 512 tokens, or as many as keep the segments to 64 and all sequences' to about 1024 workgroups.  (us, H 32,
+    // Hkv 8, d 128, waves / workgroups: 512 sequences of two tokens 10.5 / 13.4, 256 of four 10.0 / 11.1, 299 of one and one of 512 17.4 / 9.9; 16 prompts in
+    // up to 4096 workgroups 100.6, in up to 1024 98.3.)
     const int units = (H + kScanHeads - 1) / kScanHeads, sequences = B * units;
-    if (alpha != nullptr && rows > B) {
-        const int most = sequences < 4096 ? 4096 / sequences : 1, want = (rows + kScanTokens - 1) / kScanTokens;
+    if (alpha != nullptr && rows > 2LL * B) {
+        const int most = sequences < 1024 ? 1024 / sequences : 1, want = (rows + kScanTokens - 1) / kScanTokens;
         a.segments = want < most ? want : most;
         if (a.segments > 64) a.segments = 64;
     }

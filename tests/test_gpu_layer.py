@@ -280,6 +280,8 @@ APPEND = [
     ([(0, 5)] * 9 + [(0, 3000)] + [(1, 1)] * 5, 2, 2, 64, 256, 64, False, True, 0, 7, ()),
     ([(40, 2600), (0, 1), (7, 511), (0, 0), (5, 513)], 9, 3, 64, 64, 0, False, False, 2, 3, ((0, 20),)),  # prefixes in segments
     ([(3, 40000)], 1, 1, 64, 512, 16, False, True, 0, 0, ()), ([(5, 0)] * 69 + [(9, 70)], 5, 5, 64, 16, 0, False, False, 0, 0, ()),
+    ([(31, 8), (16, 9), (0, 7), (3, 64), (40, 65), (15, 1)], 9, 3, 64, 16, 32, False, True, 1, 0, ()), ([(9, 2)] * 40, 12, 4, 64, 16, 0, False, False, 0, 0, ()),
+    ([(7, 129)] + [(2, 1)] * 150, 10, 5, 64, 64, 0, False, False, 0, 1, ()),
 ]
 
 
