@@ -64,8 +64,8 @@ size_t gfwa_qk_norm_rope_backward_workspace_bytes(int B, int H, int Hkv, int N, 
  * q, k, wq, wk, eps, freq, rot, pos, flags: as given to gfwa_qk_norm_rope; q and k are read with GFWA_HEAD_NORM only and may be
  * NULL without it.  dQ: [B,H,N,d], dK, dV: [B,Hkv,N,d] of dtype `dt`, dense, as gfwa_backward_gqa writes them.
  * dq: [B,N,H,d], dk, dv: [B,N,Hkv,d] of dtype `dt`, strided, out (views of one packed gradient, say: their rows may interleave, but
- * share no element); dV and dv are both NULL or both given.  dwq, dwk: [d] fp32, out; each may be
- * NULL; with GFWA_HEAD_NORM only (without it they have to be NULL).  They are summed in an order that the sizes and the device alone decide.  workspace: device scratch of
+ * share no element); dV and dv are both NULL or both given.  dwq, dwk: [d] fp32, out; each may be NULL; with GFWA_HEAD_NORM only
+ * (without it they have to be NULL).  They are summed in an order that the sizes and the device alone decide.  workspace: device scratch of
  * at least gfwa_qk_norm_rope_backward_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after; may
  * be NULL where dwq and dwk are.
  */

@@ -196,26 +196,63 @@ struct LaneVector {
 };
 
 // The two units of a lane's row.
-// ONCE: loaded past the caches, where a load takes whole lines (bf16, D = 128).  Large inputs are read faster (us, H 32, Hkv 8, N 16384: forward 84 -> 81,
-// backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8), those that are small enough to be held from their
-// making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
-template <typename T, int D>
-constexpr bool kWholeLines = sizeof(T) == 2 && D == 128;
+// ONCE: loaded past the caches (bf16, where a load takes whole lines).  Large inputs are read faster (us, H 32, Hkv 8, d 128, N 16384: forward 84 -> 81,
+// backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8; B 4, H 16, N 4096, d 64 43.2 -> 40.6), those that are small
+// enough to be held from their making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
 constexpr long long kOnceBytes = 40 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
 template <typename T, int D, bool ONCE = false>
 struct LaneRow {
+    static constexpr bool kPair = sizeof(T) == 2 && D == 64;
     Unit8<T> a, b;
-    __device__ __forceinline__ void load(const T* row, const LaneOfRow<D>& l) {
-        a.template load<ONCE && kWholeLines<T, D>>(row + l.a);
-        b.template load<ONCE && kWholeLines<T, D>>(row + l.b);
+    // row(s): the row of the lanes with the same place in their rows and side s.
+    // kPair: rows of 128 bytes, of which a load of one unit by a row's four lanes takes half a line.  So the rows of sides 2 i and 2 i + 1 are loaded and stored
+    // one after the other, each by the lanes of both, unit a by the even side's and b by the odd one's, and arrive() gives every lane its own row's (us, halves /
+    // whole lines: forward of B 4, H 16, Hkv 4, d 64, N 4200 29.6 / 24.3, of H 32, Hkv 4, N 16384 40.6 / 32.4, backward of N 4096 36.0 / 33.5, append of 40000
+    // tokens 69.5 / 60.3; N 2048, 25 MB, forward 11.9 / 12.3).
+    template <typename Row>
+    __device__ __forceinline__ void load(Row&& row, int side, const LaneOfRow<D>& l) {
+        if constexpr (kPair) {
+            const int at = l.a + (side & 1) * (l.b - l.a);
+            a.template load<ONCE>(row(side & ~1) + at);
+            b.template load<ONCE>(row(side | 1) + at);
+        } else {
+            const T* const own = row(side);
+            a.template load<ONCE>(own + l.a);
+            b.template load<ONCE>(own + l.b);
+        }
+    }
+    __device__ __forceinline__ void arrive() {
+        if constexpr (kPair) exchange();
     }
     // PAST: stored past the caches, for what nothing reads soon.  (The cache's new rows: 16 prompts 109 -> 103 us.  The results of norm and rotation would
     // cost less themselves, us, H 32, Hkv 8, N 16384: forward 85 -> 83, backward 120 -> 117, and the kernel that reads them right after more: rope
     // and attention in a row 226 -> 233, at B 4, H 16, Hkv 4, N 4096, d 64 73 -> 78, the backward and a matrix product with its result 407 -> 412.)
-    template <bool PAST = false>
-    __device__ __forceinline__ void store(T* row, const LaneOfRow<D>& l) const {
-        a.template store<PAST>(row + l.a);
-        b.template store<PAST>(row + l.b);
+    // there(s): whether side s's row is to be written.  Called once a row; arrived: after arrive()
+    template <bool PAST, typename Row, typename There>
+    __device__ __forceinline__ void store(Row&& row, There&& there, int side, const LaneOfRow<D>& l, bool arrived = true) {
+        if constexpr (kPair) {
+            if (arrived) exchange();
+            const int at = l.a + (side & 1) * (l.b - l.a);
+            if (there(side & ~1)) a.template store<PAST>(row(side & ~1) + at);
+            if (there(side | 1)) b.template store<PAST>(row(side | 1) + at);
+        } else if (there(side)) {
+            T* const own = row(side);
+            a.template store<PAST>(own + l.a);
+            b.template store<PAST>(own + l.b);
+        }
+    }
+    // unit a of the odd side's lanes with unit b of the even one's, four lanes away
+    __device__ __forceinline__ void exchange() {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 x = __builtin_bit_cast(i32x4, a.v), y = __builtin_bit_cast(i32x4, b.v);
+        i32x4 u, v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            u[e] = __builtin_amdgcn_update_dpp(x[e], y[e], 0x114, 0xf, 0xa, false);  // row_shr:4, into lanes 4..7 and 12..15
+            v[e] = __builtin_amdgcn_update_dpp(y[e], x[e], 0x104, 0xf, 0x5, false);  // row_shl:4, into lanes 0..3 and 8..11
+        }
+        a.v = __builtin_bit_cast(bf16x8, u);
+        b.v = __builtin_bit_cast(bf16x8, v);
     }
     // norm (with weights w) and rotation
     __device__ __forceinline__ void norm_and_turn(const LaneOfRow<D>& l, bool norm, float eps, const LaneVector<D>& w, bool rotated, bool paired,
@@ -239,8 +276,8 @@ struct LaneRow {
 
 // Heads of a token that a wave takes side by side: what it reads of a token-major tensor comes in runs of kSide rows, what it writes of a head-major one in
 // runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16640, d 128 96 / 97 / 90 / 84, backward 151 / 142 / 125 /
-// 119, of N 16384 133 / 125 / 120 / 123, of H 16, Hkv 4, N 4100 21 / 21 / 22 / 30, append of 16 prompts 114 / 108 / 101 / 105; rows of 4 lanes, B 4, H 16, Hkv 4,
-// N 4096, d 64: forward 25.4 / 23.9 / 26.1 / 27.7, backward 38.7 / 37.8 / 38.4 / 46.)
+// 119, of N 16384 133 / 125 / 120 / 123, of H 16, Hkv 4, N 4100 21 / 21 / 22 / 30, append of 16 prompts 114 / 108 / 101 / 105; rows of 4 lanes, two / four heads,
+// B 4, H 16, Hkv 4, d 64: forward of N 4096 22.4 / 20.4, of N 4200 24.3 / 26.2, of N 2048 12.3 / 13.2, backward of N 4096 33.6 / 35.9, of N 4200 37.6 / 41.3.)
 template <int D>
 constexpr int kSide = D == 128 ? 4 : 2;
 

@@ -16,6 +16,12 @@ namespace {
 
 constexpr int kRopeWaves = 4;  // waves of a workgroup, each on its own
 
+// Forward: eight heads side by side where the queries and the keys have a multiple of eight and more than 128 MiB are read; what a wave reads is then one
+// token's (us, kSide / eight: H 32, Hkv 8, d 128, N 32768 174 / 155, 16384 88 / 81, 12000 65 / 62, 8192 41.5 / 42.2, 4096 22.8 / 22.7, 1024 10.2 / 10.9;
+// B 8, H 16, N 8192, d 64 164 / 157; fp32, B 2, H 16, N 4400 100 / 93).
+constexpr int kManySide = 8;
+constexpr long long kManyBytes = 128 << 20;
+
 struct RopeArgs {
     HeadsView q, k, v;     // token-major, strided (backward: dq, dk, dv are written)
     HeadsView x_q, x_k;    // backward: the inputs
@@ -69,41 +75,54 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
             const HeadsView in = keys ? a.k : a.q;
             const T* const from = (const T*)in.data + t.in(in);
             T* const to = (T*)(keys ? a.K : a.Q) + t.dense(count, a.N) * D;
-            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * in.head, l); };
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                r.load([&](int x) __attribute__((always_inline)) { return from + min(h0 + i * HG + x, h1 - 1) * in.head; }, side, l);
+            };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             LaneVector<D> w;
             if (a.norm) w.load(keys ? a.wk : a.wq, l);
             walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
-                const int h = h0 + i * HG + side;
+                r.arrive();
                 r.norm_and_turn(l, a.norm, a.eps, w, a.rot > 0, a.paired, angles);
-                if (t.there && h < h1) r.store(to + (size_t)h * a.N * D, l);
+                r.template store<false>([&](int x) __attribute__((always_inline)) { return to + (size_t)(h0 + i * HG + x) * a.N * D; },
+                                        [&](int x) __attribute__((always_inline)) { return t.there && h0 + i * HG + x < h1; }, side, l);
             });
         }
         int h0, h1;
         if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
             const T* const from = (const T*)a.v.data + t.in(a.v);
             T* const to = (T*)a.V + t.dense(a.Hkv, a.N) * D;
-            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + min(h0 + i * HG + side, h1 - 1) * a.v.head, l); };
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                r.load([&](int x) __attribute__((always_inline)) { return from + min(h0 + i * HG + x, h1 - 1) * a.v.head; }, side, l);
+            };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
-                const int h = h0 + i * HG + side;
-                if (t.there && h < h1) r.store(to + (size_t)h * a.N * D, l);
+                r.template store<false>([&](int x) __attribute__((always_inline)) { return to + (size_t)(h0 + i * HG + x) * a.N * D; },
+                                        [&](int x) __attribute__((always_inline)) { return t.there && h0 + i * HG + x < h1; }, side, l, false);
             });
         }
     }
 }
 
-template <typename T, int D, bool ONCE>
+// By the size of the inputs (bf16): up to kOnceBytes they are read through the caches; of up to kManyBytes gradients and inputs are not, of more the inputs are,
+// and rows of four lanes are taken four side by side (us, inputs through / past the caches: H 32, Hkv 8, d 128, N 8192 63.3 / 56.4, 12000 88.8 / 82.2,
+// 16384 119 / 123; four side by side instead of two: B 8, H 16, N 8192, d 64 216 -> 207, B 4, H 16, Hkv 4, N 4096 33.6 -> 35.9).
+enum BwdSize { kSmall = 0, kMiddle = 1, kLarge = 2 };
+template <int D, int SIZE>
+constexpr int kBwdSide = D == 64 && SIZE == kLarge ? 4 : kSide<D>;
+
+template <typename T, int D, int SIZE>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const RopeArgs a) {
-    constexpr int LPR = D / 16, HG = kSide<D>, RPW = 64 / LPR / HG;
+    constexpr bool ONCE = SIZE != kSmall;
+    constexpr int LPR = D / 16, HG = kBwdSide<D, SIZE>, RPW = 64 / LPR / HG;
     __shared__ float sums[kRopeWaves][2][16][64 + LPR];  // of each lane's elements, for the queries' and the keys' weights (LPR: rows do not meet in a bank)
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const LaneOfRow<D> l(lane % LPR, a.rot, a.paired);
 #pragma unroll
     for (int i = 0; i < 32; ++i) sums[wv][i >> 4][i & 15][lane] = 0.f;
     struct Rows {
-        LaneRow<T, D, ONCE> g;  // (the inputs past the caches too: 123 us against 120 at H 32, Hkv 8, N 16384, d 128)
-        LaneRow<T, D> x;
+        LaneRow<T, D, ONCE> g;
+        LaneRow<T, D, SIZE == kMiddle> x;
     };
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
@@ -125,9 +144,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
             T* const to = (T*)out.data + t.in(out);
             const T* const xs = a.norm ? (const T*)in.data + t.in(in) : nullptr;
             auto load = [&](Rows& r, int i) __attribute__((always_inline)) {
-                const int h = min(h0 + i * HG + side, h1 - 1);
-                r.g.load(from + (size_t)h * a.N * D, l);
-                if (a.norm) r.x.load(xs + h * in.head, l);
+                r.g.load([&](int x) __attribute__((always_inline)) { return from + (size_t)min(h0 + i * HG + x, h1 - 1) * a.N * D; }, side, l);
+                if (a.norm) r.x.load([&](int x) __attribute__((always_inline)) { return xs + min(h0 + i * HG + x, h1 - 1) * in.head; }, side, l);
             };
             HeadWalk<Rows, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             LaneVector<D> w, dw;
@@ -138,11 +156,13 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
                 const int h = h0 + i * HG + side;
                 const bool there = t.there && h < h1;
                 float g[8], f[8];
+                r.g.arrive();
                 r.g.a.get(g);
                 r.g.b.get(f);
                 if (a.rot > 0) angles.turn<D, true>(l, a.paired, g, f);
                 if (a.norm) {
                     float x[8], y[8];
+                    r.x.arrive();
                     r.x.a.get(x);
                     r.x.b.get(y);
                     const float rstd = row_rstd<D>(x, y, a.eps);
@@ -166,7 +186,8 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
                 }
                 r.g.a.set(g);
                 r.g.b.set(f);
-                if (there) r.g.store(to + h * out.head, l);
+                r.g.template store<false>([&](int x) __attribute__((always_inline)) { return to + (h0 + i * HG + x) * out.head; },
+                                          [&](int x) __attribute__((always_inline)) { return t.there && h0 + i * HG + x < h1; }, side, l);
             });
             if (a.part != nullptr) {  // the lane's own cells
 #pragma unroll
@@ -180,11 +201,13 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
         if (a.V != nullptr && range.part(a.H + a.Hkv, a.Hkv, h0, h1)) {
             const T* const from = (const T*)a.V + t.dense(a.Hkv, a.N) * D;
             T* const to = (T*)a.v.data + t.in(a.v);
-            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) { r.load(from + (size_t)min(h0 + i * HG + side, h1 - 1) * a.N * D, l); };
+            auto load = [&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
+                r.load([&](int x) __attribute__((always_inline)) { return from + (size_t)min(h0 + i * HG + x, h1 - 1) * a.N * D; }, side, l);
+            };
             HeadWalk<LaneRow<T, D, ONCE>, decltype(load)> walk(0, (h1 - h0 + HG - 1) / HG, load);
             walk.run([&](LaneRow<T, D, ONCE>& r, int i) __attribute__((always_inline)) {
-                const int h = h0 + i * HG + side;
-                if (t.there && h < h1) r.store(to + h * a.v.head, l);
+                r.template store<false>([&](int x) __attribute__((always_inline)) { return to + (h0 + i * HG + x) * a.v.head; },
+                                        [&](int x) __attribute__((always_inline)) { return t.there && h0 + i * HG + x < h1; }, side, l, false);
             });
         }
     }
@@ -225,12 +248,6 @@ __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __re
 // two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 122 / 124, B 4, H 16, N 8192 207 /
 // 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 27 / 22 / 22).
 constexpr int kMostSums = 768, kManySums = 512;
-
-// Forward: eight heads side by side where the queries and the keys have a multiple of eight and more than 128 MiB are read; what a wave reads is then one
-// token's (us, kSide / eight: H 32, Hkv 8, d 128, N 32768 174 / 155, 16384 88 / 81, 12000 65 / 62, 8192 41.5 / 42.2, 4096 22.8 / 22.7, 1024 10.2 / 10.9;
-// B 8, H 16, N 8192, d 64 164 / 157; fp32, B 2, H 16, N 4400 100 / 93).
-constexpr int kManySide = 8;
-constexpr long long kManyBytes = 128 << 20;
 
 long long share_out(RopeArgs& a, int D, int side) {
     a.shares = Shares((int)(((long long)a.tokens * side + 1024 / D - 1) / (1024 / D)), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
@@ -275,13 +292,11 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
     auto of_side = [&](auto side) {
-        constexpr int HG128 = decltype(side)::value ? kManySide : kSide<128>, HG64 = decltype(side)::value ? kManySide : kSide<64>;
-        if (bf16) {
-            if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true, HG128>) : launch(qk_norm_rope_kernel<bf16_t, 128, decltype(side)::value, HG128>);  // (eight: always ONCE)
-            else launch(qk_norm_rope_kernel<bf16_t, 64, false, HG64>);
-        } else {
-            d == 128 ? launch(qk_norm_rope_kernel<float, 128, false, HG128>) : launch(qk_norm_rope_kernel<float, 64, false, HG64>);
-        }
+        constexpr bool eight = decltype(side)::value;  // (then always ONCE)
+        constexpr int HG128 = eight ? kManySide : kSide<128>, HG64 = eight ? kManySide : kSide<64>;
+        if (!bf16) d == 128 ? launch(qk_norm_rope_kernel<float, 128, false, HG128>) : launch(qk_norm_rope_kernel<float, 64, false, HG64>);
+        else if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true, HG128>) : launch(qk_norm_rope_kernel<bf16_t, 128, eight, HG128>);
+        else once ? launch(qk_norm_rope_kernel<bf16_t, 64, true, HG64>) : launch(qk_norm_rope_kernel<bf16_t, 64, eight, HG64>);
     };
     many ? of_side(std::true_type{}) : of_side(std::false_type{});
     return hipGetLastError();
@@ -297,17 +312,20 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.x_q = q;
     a.x_k = k;
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
-    const long long blocks = share_out(a, d, d == 128 ? kSide<128> : kSide<64>);
+    const long long bytes = (long long)a.tokens * (H + 2LL * Hkv) * d * 2;
+    const int size = !bf16 || bytes <= kOnceBytes ? kSmall : bytes <= kManyBytes ? kMiddle : kLarge;
+    const long long blocks = share_out(a, d, d == 128 ? kSide<128> : size == kLarge ? kBwdSide<64, kLarge> : kSide<64>);
     {
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
-        if (bf16) {
-            const bool once = (long long)a.tokens * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
-            if (d == 128) once ? launch(qk_norm_rope_bwd_kernel<bf16_t, 128, true>) : launch(qk_norm_rope_bwd_kernel<bf16_t, 128, false>);
-            else launch(qk_norm_rope_bwd_kernel<bf16_t, 64, false>);
-        } else {
-            d == 128 ? launch(qk_norm_rope_bwd_kernel<float, 128, false>) : launch(qk_norm_rope_bwd_kernel<float, 64, false>);
-        }
+        auto of_size = [&](auto D) {
+            constexpr int d = decltype(D)::value;
+            if (!bf16) launch(qk_norm_rope_bwd_kernel<float, d, kSmall>);
+            else if (size == kSmall) launch(qk_norm_rope_bwd_kernel<bf16_t, d, kSmall>);
+            else if (size == kMiddle) launch(qk_norm_rope_bwd_kernel<bf16_t, d, kMiddle>);
+            else launch(qk_norm_rope_bwd_kernel<bf16_t, d, kLarge>);
+        };
+        d == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
     }
     if (a.part != nullptr) {
         ProfScope prof(kKernNormWeightSum, s);

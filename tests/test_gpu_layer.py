@@ -148,6 +148,36 @@ def test_large_inputs_as_small_ones(g, H, Hkv, N, d, dtype):
             assert all(torch.equal(a[:, :, at], b) for a, b in zip(whole, part)), i
 
 
+@pytest.mark.parametrize("H,Hkv,N,d", [(8, 8, 22223, 128), (16, 8, 33335, 64), (7, 7, 40001, 64), (5, 5, 20003, 128), (3, 1, 70007, 64)])
+def test_large_gradients_as_small_ones(g, H, Hkv, N, d):
+    """The derivative of 45 to 137 MB of inputs: the bits of calls for a part of the tokens, and the weights' gradients to the tolerance of the small ones
+    (no chain is longer: eight heads of a lane, five items of a wave; the rest in fp64)."""
+    gen = torch.Generator(device=DEV).manual_seed(N)
+    mk = lambda *s: torch.randn(s, device=DEV, generator=gen).bfloat16()
+    x, dx = mk(1, N, H + 2 * Hkv, d), torch.zeros(1, N, H + 2 * Hkv, d, device=DEV, dtype=torch.bfloat16)
+    assert x.numel() * 2 > 40 << 20
+    parts = lambda t: (t[:, :, :H], t[:, :, H:H + Hkv], t[:, :, H + Hkv:])
+    q, k, _ = parts(x)
+    dQ, dK, dV = mk(1, H, N, d), mk(1, Hkv, N, d), mk(1, Hkv, N, d)
+    w = 1 + 0.3 * torch.randn(2, d, device=DEV, generator=gen)
+    f = dev64(freq_of(d))
+    outs = parts(dx)
+    dw = g.gfwa_qk_norm_rope_backward(q, k, dQ, dK, dV, w[0], w[1], EPS, f, dq=outs[0], dk=outs[1], dv=outs[2])[3:]
+    for i in range(0, N, 6000):
+        at = slice(i, min(i + 6000, N))
+        pos = torch.arange(at.start, at.stop, dtype=torch.int32, device=DEV)[None]
+        part = g.gfwa_qk_norm_rope_backward(q[:, at], k[:, at], *(t[:, :, at].contiguous() for t in (dQ, dK, dV)), w[0], w[1], EPS, f, pos=pos)
+        assert all(torch.equal(a[:, at], b) for a, b in zip(outs, part)), i
+    for i, (y, dy) in enumerate(((q, dQ), (k, dK))):
+        y, back = y.double(), dy.double().transpose(1, 2)
+        u = y * (y * y).mean(-1, keepdim=True).add(EPS).rsqrt()
+        angle = torch.arange(N, device=DEV, dtype=torch.float64)[:, None] * f
+        c, s = angle.cos()[None, :, None], angle.sin()[None, :, None]
+        lo, hi = back[..., :d // 2], back[..., d // 2:]
+        terms = torch.cat((lo * c + hi * s, hi * c - lo * s), -1) * u
+        assert ((dw[i].double() - terms.sum((0, 1, 2))).abs() <= 160 * U * (torch.cat((lo.abs() + hi.abs(),) * 2, -1) * u.abs()).sum((0, 1, 2))).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("B,H,Hkv,N,d,rot,paired,norm,kind,pos_kind", ROPE)
 def test_norm_and_rotation_backward(g, B, H, Hkv, N, d, rot, paired, norm, kind, pos_kind, dtype):
