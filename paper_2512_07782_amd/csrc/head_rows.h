@@ -200,15 +200,15 @@ struct LaneVector {
 // backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8; B 4, H 16, N 4096, d 64 43.2 -> 40.6), those that are small
 // enough to be held from their making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
 constexpr long long kOnceBytes = 40 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
-template <typename T, int D, bool ONCE = false>
+template <typename T, int D, bool ONCE = false, bool PAIR = true>
 struct LaneRow {
-    static constexpr bool kPair = sizeof(T) == 2 && D == 64;
+    static constexpr bool kPair = sizeof(T) == 2 && D == 64 && PAIR;
     Unit8<T> a, b;
     // row(s): the row of the lanes with the same place in their rows and side s.
     // kPair: rows of 128 bytes, of which a load of one unit by a row's four lanes takes half a line.  So the rows of sides 2 i and 2 i + 1 are loaded and stored
     // one after the other, each by the lanes of both, unit a by the even side's and b by the odd one's, and arrive() gives every lane its own row's (us, halves /
-    // whole lines: forward of B 4, H 16, Hkv 4, d 64, N 4200 29.6 / 24.3, of H 32, Hkv 4, N 16384 40.6 / 32.4, backward of N 4096 36.0 / 33.5, append of 40000
-    // tokens 69.5 / 60.3; N 2048, 25 MB, forward 11.9 / 12.3).
+    // whole lines: forward of B 4, H 16, Hkv 4, d 64, N 4200 29.6 / 24.3, of H 32, Hkv 4, N 16384 40.6 / 32.4, gradients of N 4200 43.9 / 37.3, append of 40000
+    // tokens 69.5 / 60.3; N 2048, 25 MB, forward 11.9 / 12.3).  PAIR false: not worth it, for the derivative's inputs through the caches.
     template <typename Row>
     __device__ __forceinline__ void load(Row&& row, int side, const LaneOfRow<D>& l) {
         if constexpr (kPair) {

@@ -104,10 +104,12 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
     }
 }
 
-// By the size of the inputs (bf16): up to kOnceBytes they are read through the caches; of up to kManyBytes gradients and inputs are not, of more the inputs are,
-// and rows of four lanes are taken four side by side (us, inputs through / past the caches: H 32, Hkv 8, d 128, N 8192 63.3 / 56.4, 12000 88.8 / 82.2,
-// 16384 119 / 123; four side by side instead of two: B 8, H 16, N 8192, d 64 216 -> 207, B 4, H 16, Hkv 4, N 4096 33.6 -> 35.9).
-enum BwdSize { kSmall = 0, kMiddle = 1, kLarge = 2 };
+// By the size of the inputs (bf16): of more than kOnceBytes gradients are read past the caches; between kInputsBytes and kManyBytes the inputs too (three tensors of
+// that size pass the memory-side cache); of more than kManyBytes rows of four lanes are taken four side by side.  (us, inputs through / past the caches: H 32,
+// Hkv 8, d 128, N 6000, 74 MB, 42.7 / 44.9, 8192 63.3 / 56.4, 12000, that no cache holds, 88.7 / 89.4, 16384 119 / 123; H 32, Hkv 4, N 16384, d 64, 84 MB, 58.4 / 49.6, B 4, H 16,
+// Hkv 4, N 4096 33.0 / 34.0; four side by side instead of two: B 8, H 16, N 8192, d 64 216 -> 207, N 4096 33.6 -> 35.9.)
+enum BwdSize { kSmall = 0, kMiddle = 1, kSpread = 2, kLarge = 3 };
+constexpr long long kInputsBytes = 72 << 20;
 template <int D, int SIZE>
 constexpr int kBwdSide = D == 64 && SIZE == kLarge ? 4 : kSide<D>;
 
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_bwd_kernel(const
     for (int i = 0; i < 32; ++i) sums[wv][i >> 4][i & 15][lane] = 0.f;
     struct Rows {
         LaneRow<T, D, ONCE> g;
-        LaneRow<T, D, SIZE == kMiddle> x;
+        LaneRow<T, D, SIZE == kSpread, SIZE == kSpread> x;
     };
     Frequencies freq;
     if (a.rot > 0) freq.load(l, a.freq);
@@ -313,7 +315,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.x_k = k;
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
     const long long bytes = (long long)a.tokens * (H + 2LL * Hkv) * d * 2;
-    const int size = !bf16 || bytes <= kOnceBytes ? kSmall : bytes <= kManyBytes ? kMiddle : kLarge;
+    const int size = !bf16 || bytes <= kOnceBytes ? kSmall : bytes <= kInputsBytes ? kMiddle : bytes <= kManyBytes ? kSpread : kLarge;
     const long long blocks = share_out(a, d, d == 128 ? kSide<128> : size == kLarge ? kBwdSide<64, kLarge> : kSide<64>);
     {
         ProfScope prof(kKernNormRopeBwd, s);
@@ -323,6 +325,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
             if (!bf16) launch(qk_norm_rope_bwd_kernel<float, d, kSmall>);
             else if (size == kSmall) launch(qk_norm_rope_bwd_kernel<bf16_t, d, kSmall>);
             else if (size == kMiddle) launch(qk_norm_rope_bwd_kernel<bf16_t, d, kMiddle>);
+            else if (size == kSpread) launch(qk_norm_rope_bwd_kernel<bf16_t, d, kSpread>);
             else launch(qk_norm_rope_bwd_kernel<bf16_t, d, kLarge>);
         };
         d == 128 ? of_size(std::integral_constant<int, 128>{}) : of_size(std::integral_constant<int, 64>{});
