@@ -104,10 +104,11 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
     }
 }
 
-// By the size of the inputs (bf16): of more than kOnceBytes gradients are read past the caches; between kInputsBytes and kManyBytes the inputs too (three tensors of
-// that size pass the memory-side cache); of more than kManyBytes rows of four lanes are taken four side by side.  (us, inputs through / past the caches: H 32,
-// Hkv 8, d 128, N 6000, 74 MB, 42.7 / 44.9, 8192 63.3 / 56.4, 12000, that no cache holds, 88.7 / 89.4, 16384 119 / 123; H 32, Hkv 4, N 16384, d 64, 84 MB, 58.4 / 49.6, B 4, H 16,
-// Hkv 4, N 4096 33.0 / 34.0; four side by side instead of two: B 8, H 16, N 8192, d 64 216 -> 207, N 4096 33.6 -> 35.9.)
+// By the size of the inputs (bf16): of more than kOnceBytes gradients are read past the caches; between kInputsBytes and kManyBytes the inputs too (three
+// tensors of that size pass the memory-side cache); of more than kManyBytes rows of four lanes are taken four side by side.  (us, inputs through / past the
+// caches: H 32, Hkv 8, d 128, N 6000, 74 MB, 42.7 / 44.9, 8192 63.3 / 56.4, 12000, that no cache holds, 88.7 / 89.4, 16384 119 / 123; d 64, H 32, Hkv 4,
+// N 16384, 84 MB, 58.4 / 49.6, B 4, H 16, Hkv 4, N 4096 33.0 / 34.0; four side by side instead of two: B 8, H 16, N 8192 216 -> 207, B 4, H 16, Hkv 4,
+// N 4096 33.6 -> 35.9.)
 enum BwdSize { kSmall = 0, kMiddle = 1, kSpread = 2, kLarge = 3 };
 constexpr long long kInputsBytes = 72 << 20;
 template <int D, int SIZE>
