@@ -75,10 +75,11 @@ template <typename T, int D>
 struct Tile;
 
 // bf16 (16x16x32): two units make the 32 keys of the second product.  V^T goes through LDS, which hands out transposed pieces in P's order, 16-byte chunks
-// permuted so that neither the row-wise writes nor the transposed reads meet in a bank.  A weight enters the product as two bf16 numbers, itself rounded and the
+// permuted so that neither the row-wise writes nor the transposed reads meet in a bank.  A weight enters the product as two bf16 numbers, cut off and the
 // rest, off by 2^-16 of it at most: one alone would be off by 2^-8, as much as the output's own rounding (against fp64, norm of the difference 1.9e-3 to
-// 2.6e-3 instead of 1.7e-3; 64 sequences, w 1024, 46.6 us either way, one 7.9 and 7.8).  The matrix cores take 384 of the about 1700 cycles that a
-// compute unit's share of the memory's rate gives the tile's 16 KiB (D = 128).
+// 2.6e-3 instead of 1.7e-3; 64 sequences, w 1024, 46.6 us either way, one 7.9 and 7.8).  Neither part is negative, and the rest of a weight that is not zero is not
+// zero either (2^-133 at least): an infinity among the values stays one, where the rest of a rounded weight would make 0 inf or inf - inf of it.  The matrix cores
+// take 384 of the about 1700 cycles that a compute unit's share of the memory's rate gives the tile's 16 KiB (D = 128).
 template <int D>
 struct Tile<bf16_t, D> {
     static constexpr int kUnits = 2, kLds = 32 * D * 2;
@@ -133,12 +134,17 @@ struct Tile<bf16_t, D> {
     __device__ __forceinline__ Values values() const { return {}; }
     static __device__ __forceinline__ void add(f32x4 (&acc)[DT], const f32x4 (&p)[kUnits], const Values&, const char* lds, int lane) {
         const int g = lane >> 4, hd = lane & 15;
-        bf16x8 w, rest;
+        typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+        u16x8 cut;
+        bf16x8 left;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            w[e] = (bf16_t)p[e / 4][e % 4];
-            rest[e] = (bf16_t)(p[e / 4][e % 4] - (float)w[e]);
+            const float x = p[e / 4][e % 4];
+            cut[e] = (unsigned short)(__float_as_uint(x) >> 16);
+            left[e] = (bf16_t)(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u));
         }
+        const bf16x8 w = __builtin_bit_cast(bf16x8, cut);
+        const bf16x8 rest = __builtin_bit_cast(bf16x8, __builtin_elementwise_max(__builtin_bit_cast(u16x8, left), __builtin_elementwise_min(cut, (u16x8)1)));
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
