@@ -96,6 +96,7 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfw
  * alpha: fp32, gate of head h of row n at alpha[n * alpha_token + h * alpha_head] (strides of at least 0, offsets below 2^40);  NULL: cp is left
  * alone and may be NULL.
  * start: [B+1], cached: [B] int32 in device memory, start not decreasing, cached >= 0 (a sequence may have no new token).
+ * Rows 0 .. rows-1 alone are there: where start begins in front of row 0 or ends behind the last row, the others' tokens are passed over.
  * Rows that belong to no sequence (in front of start[0], from start[B] on) are left out: their rows of Q stay as they were.  Of rows whose
  * position lies outside the table, or in a page that is not there, the query alone is written.
  * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page.

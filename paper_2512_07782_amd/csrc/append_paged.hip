@@ -86,15 +86,16 @@ constexpr int kScanHeads = 8;    // heads that are taken together
 constexpr int kScanGroups = 8;   // groups of 64 tokens whose gates are on their way together
 constexpr int kScanTokens = 64 * kScanGroups;
 
-// A sequence's new rows n0 .. n1, and how many tokens its cache holds.
+// A sequence's new rows n0 .. n1, how many tokens its cache holds, and the position of row 0, were it the sequence's.
 struct NewTokens {
     int n0, n1;
-    long long before;
+    long long before, origin;
     __device__ __forceinline__ NewTokens(const AppendArgs& a, int b) {
         const int from = a.start[b], to = a.start[b + 1];
         n0 = min(max(from, 0), a.rows);
         n1 = min(max(to, n0), a.rows);
         before = a.cached[b];
+        origin = before - from;
     }
 };
 
@@ -117,7 +118,7 @@ __device__ __forceinline__ void prefix_heads(const AppendArgs& a, int b, const N
 #pragma unroll
         for (int u = 0; u < GROUPS; ++u) {  // (no condition at a load: all are on their way before the first one is waited for)
             const int t = min(n + 64 * u + lane, to - 1);
-            const long long p = s.before + (t - s.n0);
+            const long long p = s.origin + t;
             const int at = (int)max(0LL, min(p, last)), i = at / a.page;
             row[u] = at - i * a.page;
             id[u] = a.table[(size_t)b * a.max_pages + i];
@@ -144,7 +145,7 @@ __device__ void prefix_few(const AppendArgs& a, int b, const NewTokens& s, int h
     const int lane = threadIdx.x & 63, t = lane / kScanHeads, h = h0 + lane % kScanHeads;
     const bool mine = s.n0 + t < s.n1 && h < a.H;
     int at = 0;
-    const int id = mine ? page_of(a, b, s.before + t, at) : -1;
+    const int id = mine ? page_of(a, b, s.origin + s.n0 + t, at) : -1;
     double c = mine ? a.alpha[(s.n0 + t) * a.alpha_token + h * a.alpha_head] : 0.f;
     if (s.n1 - s.n0 > 1) {
 #pragma unroll

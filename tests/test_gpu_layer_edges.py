@@ -50,3 +50,35 @@ def test_decode_infinities_among_the_values(g, scores, T, w, H, Hkv, d, dtype):
     assert got[..., 20].isnan().all()
     want[..., 20] = got[..., 20] = 0
     assert torch.equal(got, want), (got != want).nonzero()[:5]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens", [[9], [3, 5, 40], [700, 30], [20] + [1] * 40, [2] + [1] * 9, [2600, 1, 0, 77]])
+@pytest.mark.parametrize("ahead", [1, 37])
+def test_append_of_a_batch_that_begins_in_front_of_row_0(g, ahead, lens, dtype):
+    """start[0] = -ahead: the first sequence's tokens in front of row 0 are not here, those from row 0 on stand `ahead` positions further on, and their
+    prefix follows the cached one.  Keys, values and prefixes meet in the same slots; the last rows of the batch are not here either."""
+    H, Hkv, d, page = 9, 3, 64, 16
+    cached = [50] + [(7 * b) % 45 for b in range(1, len(lens))]
+    rng, table, Kp, Vp, cp = paged_case(41, [(c + ahead * (b == 0), n) for b, (c, n) in enumerate(zip(cached, lens))], H, Hkv, d, page, dtype)
+    for i in range(50, 50 + ahead):  # what stands in front of the first row is the prefix of position 49
+        cp[table[0, i // page], :, i % page] = cp[table[0, 49 // page], :, 49 % page]
+    start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    behind = min(2, lens[-1])
+    rows = int(start[-1]) - behind
+    there = np.minimum(start, rows)
+    q, k, v = (store(rng.standard_normal((rows, h, d)), dtype) for h in (H, Hkv, Hkv))
+    alpha = (rng.random((rows, H)) * 0.3).astype(np.float32)
+    (Kp, tK), (Vp, tV), tc = store(Kp, dtype), store(Vp, dtype), gpu(cp)
+    Q0, tQ = store(rng.standard_normal((rows, H, d)), dtype)
+    given = start.copy()
+    given[0] -= ahead
+    g.gfwa_append_paged(k[1], v[1], tK, tV, gpu(given), gpu(np.array(cached, dtype=np.int32)), gpu(table), q=q[1], norm=False, alpha=gpu(alpha), cp=tc, Q=tQ)
+    cached[0] += ahead
+    Qr, Kr, Vr, cr = ol.append_paged(q[0], k[0], v[0], None, None, EPS, False, None, False, alpha, there, cached, table, Q0, Kp, Vp, cp)
+    for name, a, b in (("Q", tQ, Qr), ("K", tK, Kr), ("V", tV, Vr)):  # no arithmetic
+        assert np.array_equal(host(a), b, equal_nan=True), name
+    got = host(tc)
+    assert np.array_equal(np.isnan(got), np.isnan(cr))
+    fin = ~np.isnan(cr)
+    assert (np.abs(got[fin] - cr[fin]) <= U * np.abs(cr[fin])).all()
