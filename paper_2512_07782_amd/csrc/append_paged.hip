@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const A
                 p = before + (n - first);
                 if (range.x1 > keys) id = page_of(a, b, p, row);
             }
-            if (turned) angles.at(l, (int)p, freq);
+            if (turned) angles.at(l, (double)p, freq);
         };
         auto heads_of = [&](const HeadsView& in, const float* weight, void* out, int first, int count, auto kind) __attribute__((always_inline)) {
             constexpr HeadKind K = decltype(kind)::value;

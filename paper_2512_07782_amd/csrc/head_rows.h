@@ -87,10 +87,10 @@ struct LaneOfRow {
 };
 
 // cos and sin of p * freq.  The angle in half turns, fp64, is brought into one turn before it becomes fp32: to 2^-25 half turns,
-// wherever p stands, plus the fp64 product's own rounding (2^-53 of the whole angle).
-__device__ __forceinline__ void cos_sin_of(int p, double freq, float& c, float& s) {
+// wherever p stands, plus what three roundings in fp64 (1/pi, freq / pi and its product with p) leave of the whole angle, 3 * 2^-53 of it.
+__device__ __forceinline__ void cos_sin_of(double p, double freq, float& c, float& s) {
     constexpr double kInvPi = 0.31830988618379067154;
-    double t = (double)p * (freq * kInvPi);
+    double t = p * (freq * kInvPi);
     t = fma(-2.0, rint(0.5 * t), t);
     sincospif((float)t, &s, &c);
 }
@@ -111,11 +111,11 @@ struct Frequencies {
     }
 };
 
-// The eight angles of a lane at position p.
+// The eight angles of a lane at position p (a whole number; new tokens of a cache may stand past 2^31).
 struct Angles {
     float c[8], s[8];
     template <int D>
-    __device__ __forceinline__ void at(const LaneOfRow<D>& l, int p, const Frequencies& f) {
+    __device__ __forceinline__ void at(const LaneOfRow<D>& l, double p, const Frequencies& f) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool turn = e < 4 ? l.turn_a : l.turn_b;

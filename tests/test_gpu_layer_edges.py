@@ -82,3 +82,25 @@ def test_append_of_a_batch_that_begins_in_front_of_row_0(g, ahead, lens, dtype):
     assert np.array_equal(np.isnan(got), np.isnan(cr))
     fin = ~np.isnan(cr)
     assert (np.abs(got[fin] - cr[fin]) <= U * np.abs(cr[fin])).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("paired", [False, True])
+def test_append_rotates_queries_past_the_largest_position(g, paired, dtype):
+    """Positions from 2^31 on are outside every table, but their queries are written, rotated by where they stand."""
+    H, Hkv, d, page, n = 4, 2, 64, 16, 21
+    rng, table, Kp, Vp, cp = paged_case(43, [(16, 0)], H, Hkv, d, page, dtype)
+    cached = np.array([2 ** 31 - 10], dtype=np.int32)
+    q, tq = store(rng.standard_normal((n, H, d)), dtype)
+    (k, tk), (v, tv), tK, tV, tc = store(q[:, :Hkv], dtype), store(q[:, :Hkv], dtype), store(Kp, dtype)[1], store(Vp, dtype)[1], gpu(cp)
+    before, freq = tK.clone(), freq_of(d)
+    Q = g.gfwa_append_paged(tk, tv, tK, tV, gpu(np.array([0, n], dtype=np.int32)), gpu(cached), gpu(table), q=tq, freq=dev64(freq), norm=False, paired=paired,
+                            alpha=gpu(np.ones((n, H), dtype=np.float32)), cp=tc)
+    pos = 2 ** 31 - 10 + np.arange(n, dtype=np.int64)
+    ref = ol.norm_rope_rows(q, None, EPS, False, pos, freq, paired)
+    off = 32 * U + 2.0 ** -51 * pos.max()
+    i, j = ol._pairs(d, d, paired)
+    both = np.zeros(q.shape)
+    both[..., i] = both[..., j] = np.abs(q[..., i]) + np.abs(q[..., j])
+    assert (np.abs(host(Q) - ref) <= HALF[dtype] * np.abs(ref) + off * both * (1 + HALF[dtype])).all()
+    assert np.array_equal(host(tK), host(before), equal_nan=True) and np.array_equal(host(tc), cp.astype(np.float64), equal_nan=True)
