@@ -4,8 +4,8 @@
  * key/value cache for serving.  Part of libgfwa; the conventions of gfwa.h hold (device pointers, the caller's stream,
  * status codes, nothing allocated, nothing launched on an error) except where a strided layout is named.  What a call writes
  * (outputs, cache, workspace) may not overlap what it reads, nor each other, judged by the ranges of bytes that the tensors span:
- * GFWA_ERR_OVERLAP (dq, dk and dv among each other are the one exception).  A workspace belongs to its call until that is done on the stream: calls that
- * may run at the same time (two streams, two captured graphs) need one each.
+ * GFWA_ERR_OVERLAP (dq, dk and dv among each other are the one exception: there the first and last rows of each are looked for among the others' rows).
+ * A workspace belongs to its call until that is done on the stream: calls that may run at the same time (two streams, two captured graphs) need one each.
  */
 #ifndef GFWA_LAYER_H
 #define GFWA_LAYER_H

@@ -3,6 +3,7 @@
 #include <stdint.h>
 #include <stdlib.h>
 #include <string.h>
+#include <algorithm>
 #include <atomic>
 #include <initializer_list>
 #include <mutex>
@@ -97,20 +98,39 @@ struct HeadsSpan {
     Bytes bytes(int B, int N, int d, size_t size) const {
         return t ? Bytes{t->data, (size_t)(last_row(B, N) + d) * size} : Bytes{nullptr, 0};
     }
-    // whether no two rows share an element: taken by stride, each dimension steps over all of the one below it
-    bool rows_disjoint(int B, int N, int d) const {
-        if (!t) return true;
-        long long dims[3][2] = {{t->batch, B}, {t->token, N}, {t->head, heads}};
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2 - i; ++j)
-                if (dims[j][0] > dims[j + 1][0]) std::swap(dims[j], dims[j + 1]);
-        long long reach = d;
-        for (auto& x : dims) {
-            if (x[1] == 1) continue;
-            if (x[0] < reach) return false;
-            reach += x[0] * (x[1] - 1);
+    // its dimensions by stride, the widest last, and what each reaches over
+    struct Nest {
+        long long dims[3][2];
+        Nest(const gfwa_heads_t& t, int B, int N, int heads) : dims{{t.batch, B}, {t.token, N}, {t.head, heads}} {
+            for (int i = 0; i < 2; ++i)
+                for (int j = 0; j < 2 - i; ++j)
+                    if (dims[j][0] > dims[j + 1][0]) std::swap(dims[j], dims[j + 1]);
         }
-        return true;
+        // whether no two rows share an element: taken by stride, each dimension steps over all of the one below it
+        bool disjoint(int d) const {
+            long long reach = d;
+            for (auto& x : dims) {
+                if (x[1] == 1) continue;
+                if (x[0] < reach) return false;
+                reach += x[0] * (x[1] - 1);
+            }
+            return true;
+        }
+        // whether element `at`, counted from the first one, is in a row (of disjoint ones: the last one not behind it has it, or none)
+        bool holds(long long at, int d) const {
+            if (at < 0) return false;
+            for (int i = 2; i >= 0; --i)
+                if (dims[i][1] > 1) at -= dims[i][0] * std::min(at / dims[i][0], dims[i][1] - 1);
+            return at < d;
+        }
+    };
+    bool rows_disjoint(int B, int N, int d) const { return !t || Nest(*t, B, N, heads).disjoint(d); }
+    // whether its first or last row meets a row of o, a tensor of disjoint rows
+    bool ends_meet(const HeadsSpan& o, int B, int N, int d, size_t size) const {
+        if (!t || !o.t) return false;
+        const long long first = ((intptr_t)t->data - (intptr_t)o.t->data) / (long long)size, last = first + last_row(B, N);
+        const Nest rows(*o.t, B, N, o.heads);
+        return rows.holds(first, d) || rows.holds(first + d - 1, d) || rows.holds(last, d) || rows.holds(last + d - 1, d);
     }
 };
 
@@ -375,6 +395,9 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfw
         if (int r = x.check(B, N, d, size)) return r;
         if (!x.rows_disjoint(B, N, d)) return GFWA_ERR_OVERLAP;
     }
+    for (const HeadsSpan& x : outs)
+        for (const HeadsSpan& o : outs)
+            if (&x != &o && x.ends_meet(o, B, N, d, size)) return GFWA_ERR_OVERLAP;
     const Bytes grads[] = {{dQ, bytes * H}, {dK, bytes * Hkv}, {dV, bytes * Hkv}};
     for (const Bytes& g : grads)
         if (!aligned(g.at, 16)) return GFWA_ERR_ALIGN;
