@@ -272,14 +272,14 @@ def gfwa_qk_norm_rope_backward_workspace_bytes(B: int, H: int, Hkv: int, N: int,
     return int(load_library().gfwa_qk_norm_rope_backward_workspace_bytes(B, H, Hkv, N, d))
 
 
-def gfwa_qk_norm_rope_backward(q: torch.Tensor, k: torch.Tensor, dQ: torch.Tensor, dK: torch.Tensor, dV: Optional[torch.Tensor] = None,
+def gfwa_qk_norm_rope_backward(q: Optional[torch.Tensor], k: Optional[torch.Tensor], dQ: torch.Tensor, dK: torch.Tensor, dV: Optional[torch.Tensor] = None,
                                wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
                                freq: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, norm: bool = True,
                                paired: bool = False, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                                dv: Optional[torch.Tensor] = None, dwq: Optional[torch.Tensor] = None,
                                dwk: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
-    """Derivative of gfwa_qk_norm_rope, whose arguments q .. paired are.  dQ [B,H,N,d], dK, dV [B,Hkv,N,d] dense; dq, dk, dv: strided outputs of
-    q's and k's shapes (views of one packed gradient) or None.  Returns dq, dk, dv (None without dV), dwq, dwk ([d] fp32, each None without
+    """Derivative of gfwa_qk_norm_rope, whose arguments q .. paired are (q, k: None with norm=False, where they are not read).  dQ [B,H,N,d], dK, dV
+    [B,Hkv,N,d] dense; dq, dk, dv: strided outputs of q's and k's shapes (views of one packed gradient) or None.  Returns dq, dk, dv (None without dV), dwq, dwk ([d] fp32, each None without
     its weight unless an output for it is given)."""
     return (_call or _native()).qk_norm_rope_backward(q, k, dQ, dK, dV, wq, wk, eps, freq, norm, paired, pos, dq, dk, dv, dwq, dwk, workspace)
 

@@ -562,15 +562,18 @@ struct HeadsOutput {
 
 // q, k, dQ, dK, dV, wq, wk, eps, freq, norm, paired, pos, dq, dk, dv, dwq, dwk, workspace
 PyObject* qk_norm_rope_backward(PyObject* const* a) {
-    const at::Tensor &q = tensor_of(a[0], "q"), &k = tensor_of(a[1], "k");
-    if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d]");
-    const int64_t B = q.size(0), N = q.size(1), H = q.size(2), d = q.size(3), Hkv = kv_heads(H, k.size(2));
+    const int norm = PyObject_IsTrue(a[9]);
+    if (norm < 0) throw PyError{};
+    const bool with_q = norm || a[0] != Py_None, with_k = norm || a[1] != Py_None;  // without the norm neither is read, and the gradients have their sizes
+    const at::Tensor &q = with_q ? tensor_of(a[0], "q") : tensor_of(a[2], "dQ"), &k = with_k ? tensor_of(a[1], "k") : tensor_of(a[3], "dK");
+    if (q.dim() != 4 || k.dim() != 4) fail(PyExc_ValueError, "q must be [B,N,H,d] and k [B,N,Hkv,d], dQ [B,H,N,d] and dK [B,Hkv,N,d]");
+    const int64_t B = q.size(0), N = q.size(with_q ? 1 : 2), H = q.size(with_q ? 2 : 1), d = q.size(3), Hkv = kv_heads(H, k.size(with_k ? 2 : 1));
     fits_int({B, N, H, d});
     const int dt = storage_type(q);
     const at::ScalarType st = q.scalar_type();
     const OneDevice dev(q);
     const int64_t qs[4] = {B, N, H, d}, ks[4] = {B, N, Hkv, d}, Qs[4] = {B, H, N, d}, Ks[4] = {B, Hkv, N, d}, ps[2] = {B, N}, ws[1] = {d};
-    const Heads hq(q, qs, st, dev, "q", false), hk(k, ks, st, dev, "k", false);
+    const Heads hq = with_q ? Heads(q, qs, st, dev, "q", false) : Heads(), hk = with_k ? Heads(k, ks, st, dev, "k", false) : Heads();
     const void *dQ = dense(a[2], Qs, st, dev, "dQ").const_data_ptr(), *dK = dense(a[3], Ks, st, dev, "dK").const_data_ptr();
     const void* dV = optional_input(a[4], Ks, st, dev, "dV");
     const Rotation how(a + 5, d, dev);

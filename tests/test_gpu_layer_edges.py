@@ -104,3 +104,29 @@ def test_append_rotates_queries_past_the_largest_position(g, paired, dtype):
     both[..., i] = both[..., j] = np.abs(q[..., i]) + np.abs(q[..., j])
     assert (np.abs(host(Q) - ref) <= HALF[dtype] * np.abs(ref) + off * both * (1 + HALF[dtype])).all()
     assert np.array_equal(host(tK), host(before), equal_nan=True) and np.array_equal(host(tc), cp.astype(np.float64), equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,Hkv,N,d,rot", [(1, 1, 1, 1, 64, 64), (3, 6, 2, 77, 128, 32), (2, 4, 4, 9, 64, 0)])
+def test_gradient_without_the_norm_needs_no_inputs(g, B, H, Hkv, N, d, rot, dtype):
+    """norm=False reads neither q nor k: the same bits without them, or without one of them."""
+    rng = np.random.default_rng(N)
+    q, k = (store(rng.standard_normal((B, N, h, d)), dtype)[1] for h in (H, Hkv))
+    grads = [store(rng.standard_normal((B, h, N, d)), dtype)[1] for h in (H, Hkv, Hkv)]
+    f = dev64(freq_of(rot))
+    want = g.gfwa_qk_norm_rope_backward(q, k, *grads, freq=f, norm=False)
+    assert want[0].shape == q.shape and want[1].shape == want[2].shape == k.shape
+    for a, b in ((None, None), (q, None), (None, k)):
+        got = g.gfwa_qk_norm_rope_backward(a, b, *grads, freq=f, norm=False)
+        assert all(torch.equal(x, y) for x, y in zip(got[:3], want[:3])) and got[3] is got[4] is None
+    packed = torch.full((B, N, H + 2 * Hkv, d), float("nan"), dtype=TORCH[dtype], device=DEV)
+    dq, dk, dv = packed[:, :, :H], packed[:, :, H:H + Hkv], packed[:, :, H + Hkv:]
+    g.gfwa_qk_norm_rope_backward(None, None, *grads, freq=f, norm=False, dq=dq, dk=dk, dv=dv)
+    assert all(torch.equal(x, y) for x, y in zip((dq, dk, dv), want))
+    for bad in (dict(), dict(norm=True)):
+        with pytest.raises(TypeError, match="q must be a tensor"):
+            g.gfwa_qk_norm_rope_backward(None, k, *grads, **bad)
+    with pytest.raises(ValueError, match="shape"):
+        g.gfwa_qk_norm_rope_backward(None, None, grads[0], grads[1], grads[0][:, :, :, :32], norm=False)
+    with pytest.raises(ValueError, match="shape"):
+        g.gfwa_qk_norm_rope_backward(None, None, *grads, norm=False, dq=dq.transpose(1, 2) if H != N else dk[:, :, :0])

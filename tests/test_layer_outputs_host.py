@@ -68,3 +68,19 @@ def rope_bwd_sized(lib, outs, B, N, H, Hkv, d):
     q, k = heads(0x1000000, N * H * d, H * d, d), heads(0x1800000, N * Hkv * d, Hkv * d, d)
     return lib.gfwa_qk_norm_rope_backward(0, r(q), r(k), A, A, 1e-6, A, 64, None, 1, P(0x2000000), P(0x3000000), P(0x4000000), *[r(x) for x in outs], A, P(0x20000),
                                           None, 0, B, H, Hkv, N, d, None)
+
+
+def test_gradient_without_inputs_on_the_host():
+    import torch
+    import paper_2512_07782_amd as g
+    x = torch.zeros(1, 2, 4, 64)
+    with pytest.raises(TypeError, match="q must be a tensor"):
+        g.gfwa_qk_norm_rope_backward(None, None, x, x)
+    with pytest.raises(TypeError, match="dQ must be a tensor"):
+        g.gfwa_qk_norm_rope_backward(None, None, None, x, norm=False)
+    with pytest.raises(ValueError, match="dQ .B,H,N,d."):
+        g.gfwa_qk_norm_rope_backward(None, None, x[0], x, norm=False)
+    with pytest.raises(ValueError, match="divide"):
+        g.gfwa_qk_norm_rope_backward(None, None, x, torch.zeros(1, 3, 4, 64), norm=False)
+    with pytest.raises(ValueError, match="GPU"):
+        g.gfwa_qk_norm_rope_backward(None, None, x, x, norm=False)
