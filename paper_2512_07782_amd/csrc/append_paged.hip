@@ -331,7 +331,7 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     ProfScope prof(kKernAppendPaged, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.scan_blocks + blocks)), dim3(kThreads), 0, s, a); };
     if (bf16) {
-        const bool once = rows * (H + 2LL * Hkv) * d * 2 > kOnceBytes;
+        const bool once = rows * ((Q != nullptr ? H : 0) + 2LL * Hkv) * d * 2 > kOnceBytes;  // of what is read
         if (d == 128) once ? launch(append_paged_kernel<bf16_t, 128, true>) : launch(append_paged_kernel<bf16_t, 128, false>);
         else once ? launch(append_paged_kernel<bf16_t, 64, true>) : launch(append_paged_kernel<bf16_t, 64, false>);
     } else {

@@ -199,6 +199,8 @@ struct LaneVector {
 // ONCE: loaded past the caches (bf16, where a load takes whole lines).  Large inputs are read faster (us, H 32, Hkv 8, d 128, N 16384: forward 84 -> 81,
 // backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8; B 4, H 16, N 4096, d 64 43.2 -> 40.6), those that are small
 // enough to be held from their making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
+// Forward and append count what they read (through / past the caches: append without queries, H 32, Hkv 8, d 128, 8100 tokens, 33 MB, 15.1 / 19.0,
+// forward without values, H 16, Hkv 16, N 4100, 34 MB, 14.7 / 16.7).
 constexpr long long kOnceBytes = 40 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
 template <typename T, int D, bool ONCE = false, bool PAIR = true>
 struct LaneRow {

@@ -289,13 +289,14 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     a.q = q;
     a.k = k;
     a.v = v;
-    const long long bytes = (long long)a.tokens * (H + 2LL * Hkv) * d * (bf16 ? 2 : 4);
-    const bool many = H % kManySide == 0 && Hkv % kManySide == 0 && bytes > kManyBytes, once = bytes > kOnceBytes;
+    const long long row = (long long)a.tokens * d * (bf16 ? 2 : 4);  // of one head
+    const bool many = H % kManySide == 0 && Hkv % kManySide == 0 && row * (H + 2LL * Hkv) > kManyBytes;
+    const bool once = row * (H + (V != nullptr ? 2LL : 1LL) * Hkv) > kOnceBytes;  // of what is read
     const long long blocks = share_out(a, d, many ? kManySide : d == 128 ? kSide<128> : kSide<64>);
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
     auto of_side = [&](auto side) {
-        constexpr bool eight = decltype(side)::value;  // (then always ONCE)
+        constexpr bool eight = decltype(side)::value;  // (then always ONCE: without values two thirds of kManyBytes are read at least)
         constexpr int HG128 = eight ? kManySide : kSide<128>, HG64 = eight ? kManySide : kSide<64>;
         if (!bf16) d == 128 ? launch(qk_norm_rope_kernel<float, 128, false, HG128>) : launch(qk_norm_rope_kernel<float, 64, false, HG64>);
         else if (d == 128) once ? launch(qk_norm_rope_kernel<bf16_t, 128, true, HG128>) : launch(qk_norm_rope_kernel<bf16_t, 128, eight, HG128>);

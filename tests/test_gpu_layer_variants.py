@@ -142,3 +142,28 @@ def test_weights_gradients_to_their_own_chain(g, H, Hkv, N, d):
         terms = torch.cat((lo * c + hi * s, hi * c - lo * s), -1) * u
         both = torch.cat((lo.abs() + hi.abs(),) * 2, -1) * u.abs()
         assert ((got.double() - terms.sum((0, 1, 2))).abs() <= U * ((16 + 34) * terms.abs() + 8 * both).sum((0, 1, 2))).all()
+
+
+def test_sizes_count_what_is_read(g):
+    """Keys alone, or without values: 34 MB are read of a projection of 50 MB, which the caches hold.  The same bits as with queries, or values."""
+    H, Hkv, N, d, page = 16, 16, 4100, 128, 64
+    x, f = normal(1, (1, N, H + 2 * Hkv, d)), dev64(freq_of(d))
+    q, k, v = x[:, :, :H], x[:, :, H:H + Hkv], x[:, :, H + Hkv:]
+    outs = []
+    names = kernels(lambda: outs.extend((g.gfwa_qk_norm_rope(q, k, v, freq=f), g.gfwa_qk_norm_rope(q, k, freq=f))))
+    assert all(variant("qk_norm_rope_kernel", "bf16", d, once, 4) in names for once in (True, False)), names
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and outs[1][2] is None
+    i32 = lambda y: torch.tensor(y, dtype=torch.int32, device=DEV)
+    pages = N // page + 1
+    table, alpha, caches = torch.arange(pages, device=DEV, dtype=torch.int32)[None], torch.rand(N, H, device=DEV), []
+
+    def append(**kw):
+        Kp, Vp, cp = (torch.zeros(s, dtype=t, device=DEV) for s, t in (((pages, Hkv, page, d), torch.bfloat16),) * 2 + (((pages, H, page), torch.float32),))
+        g.gfwa_append_paged(k[0], v[0], Kp, Vp, i32([0, N]), i32([0]), table, freq=f, alpha=alpha, cp=cp, **kw)
+        caches.append((Kp, Vp, cp))
+
+    names = kernels(lambda: append(q=q[0]))
+    assert variant("append_paged_kernel", "bf16", d, True) in names, names
+    names = kernels(append)
+    assert variant("append_paged_kernel", "bf16", d, False) in names, names
+    assert all(torch.equal(a, b) for a, b in zip(*caches))
