@@ -247,15 +247,16 @@ __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __re
     }
 }
 
-// Workgroups that leave sums of the weights' gradients: three waves a SIMD are there at a time (bf16), and what fits in them goes at once; more goes through
+// Workgroups that leave sums of the weights' gradients.  In bf16 three waves a SIMD are there at a time, and what fits in them goes at once; more goes through
 // two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 122 / 124, B 4, H 16, N 8192 207 /
-// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 27 / 22 / 22).
+// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 19.4 with up to 768, 23.6 with 512).  In fp32 two waves a SIMD are all there are (512 / 768 workgroups,
+// d 128: H 8, Hkv 2, N 5000 25.7 / 28.3, H 16, Hkv 4, N 6100 51.5 / 57.2, N 4200 44.5 / 44.6, H 32, Hkv 8, N 5000 83.0 / 82.2).
 constexpr int kMostSums = 768, kManySums = 512;
 
-long long share_out(RopeArgs& a, int D, int side) {
+long long share_out(RopeArgs& a, int D, int side, bool bf16) {
     a.shares = Shares((int)(((long long)a.tokens * side + 1024 / D - 1) / (1024 / D)), a.H + (a.V != nullptr ? 2 : 1) * a.Hkv, side);
     const long long blocks = ((long long)a.shares.items + kRopeWaves - 1) / kRopeWaves;
-    if (a.part != nullptr) return blocks <= kMostSums ? blocks : kManySums;
+    if (a.part != nullptr) return blocks <= (bf16 ? kMostSums : kManySums) ? blocks : kManySums;
     return blocks < 1 << 20 ? blocks : 1 << 20;
 }
 
@@ -292,7 +293,7 @@ hipError_t qk_norm_rope(bool bf16, const HeadsView& q, const HeadsView& k, const
     const long long row = (long long)a.tokens * d * (bf16 ? 2 : 4);  // of one head
     const bool many = H % kManySide == 0 && Hkv % kManySide == 0 && row * (H + 2LL * Hkv) > kManyBytes;
     const bool once = row * (H + (V != nullptr ? 2LL : 1LL) * Hkv) > kOnceBytes;  // of what is read
-    const long long blocks = share_out(a, d, many ? kManySide : d == 128 ? kSide<128> : kSide<64>);
+    const long long blocks = share_out(a, d, many ? kManySide : d == 128 ? kSide<128> : kSide<64>, bf16);
     ProfScope prof(kKernNormRope, s);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };
     auto of_side = [&](auto side) {
@@ -318,7 +319,7 @@ hipError_t qk_norm_rope_backward(bool bf16, const HeadsView& q, const HeadsView&
     a.part = dwq != nullptr || dwk != nullptr ? part : nullptr;
     const long long bytes = (long long)a.tokens * (H + 2LL * Hkv) * d * 2;
     const int size = !bf16 || bytes <= kOnceBytes ? kSmall : bytes <= kInputsBytes ? kMiddle : bytes <= kManyBytes ? kSpread : kLarge;
-    const long long blocks = share_out(a, d, d == 128 ? kSide<128> : size == kLarge ? kBwdSide<64, kLarge> : kSide<64>);
+    const long long blocks = share_out(a, d, d == 128 ? kSide<128> : size == kLarge ? kBwdSide<64, kLarge> : kSide<64>, bf16);
     {
         ProfScope prof(kKernNormRopeBwd, s);
         auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kRopeWaves), 0, s, a); };

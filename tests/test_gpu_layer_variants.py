@@ -167,3 +167,19 @@ def test_sizes_count_what_is_read(g):
     names = kernels(append)
     assert variant("append_paged_kernel", "bf16", d, False) in names, names
     assert all(torch.equal(a, b) for a, b in zip(*caches))
+
+
+@pytest.mark.parametrize("dtype,most", [("bf16", 768), ("f32", 512)])
+def test_workgroups_that_leave_sums_are_there_at_once(g, dtype, most):
+    """Each leaves one row in the workspace: as many as the type's registers let run together (four waves of three, or two, a SIMD of 256 compute units)."""
+    if torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("counts workgroups of a whole MI355X")
+    H, Hkv, N, d = 8, 2, 5900, 128
+    x = normal(1, (1, N, H + 2 * Hkv, d), dtype)
+    grads = [normal(2 + i, (1, h, N, d), dtype) for i, h in enumerate((H, Hkv, Hkv))]
+    w = normal(6, (2, d), "f32")
+    ws = torch.full((768, 2 * d), 3.5, device=DEV)
+    assert ws.nbytes >= g.gfwa_qk_norm_rope_backward_workspace_bytes(1, H, Hkv, N, d)
+    g.gfwa_qk_norm_rope_backward(x[:, :, :H], x[:, :, H:H + Hkv], *grads, w[0], w[1], freq=dev64(freq_of(d)), workspace=ws)
+    used = int((ws != 3.5).any(1).nonzero().max()) + 1
+    assert used <= most and (dtype == "f32" or used > 512), used
