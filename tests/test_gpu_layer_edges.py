@@ -130,3 +130,20 @@ def test_gradient_without_the_norm_needs_no_inputs(g, B, H, Hkv, N, d, rot, dtyp
         g.gfwa_qk_norm_rope_backward(None, None, grads[0], grads[1], grads[0][:, :, :, :32], norm=False)
     with pytest.raises(ValueError, match="shape"):
         g.gfwa_qk_norm_rope_backward(None, None, *grads, norm=False, dq=dq.transpose(1, 2) if H != N else dk[:, :, :0])
+
+
+@pytest.mark.parametrize("shape,bound", [("40,32,8,2000,128,512", "hbm"), ("2,8,2,700,64,100", "cache")])
+def test_bench_of_the_paged_step_reads_what_no_cache_holds(g, shape, bound, capsys):
+    """A rate counts against the memory's only where more than twice the memory-side cache is read between two looks at a window."""
+    import json
+    import sys
+    import bench
+    argv, sys.argv = sys.argv, ["bench.py", "--decode", shape, "--paged", "16", "--steps", "20", "--warmup", "2"]
+    try:
+        assert bench.main() == 0
+    finally:
+        sys.argv = argv
+    line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    between = line["detail"]["caches_in_turn"] * line["detail"]["algorithmic_bytes"]
+    assert line["detail"]["caches_in_turn"] >= 2 and line["roofline"]["bound"] == bound and (between >= 512 << 20) == (bound == "hbm")
+    assert line["value"] < line["roofline"]["peak"]
