@@ -100,6 +100,12 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfw
  * Rows that belong to no sequence (in front of start[0], from start[B] on) are left out: their rows of Q stay as they were.  Of rows whose
  * position lies outside the table, or in a page that is not there, the query alone is written.
  * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page.
+ *
+ * What reads Q: gfwa_decode_paged, a query for each of its rows.  In a decoding step these are the batch's; of several new tokens every one
+ * can be a row there, with its sequence's row of the table and its own position, which reads each one's window.  gfwa_forward_gqa reads no
+ * pages: a prompt goes through gfwa_qk_norm_rope and the attention, and is appended without queries, from the projection's k and v (the
+ * same bits as K and V have; rows of padding between sequences of a padded batch count as tokens and are written over by those that follow,
+ * cached being the lengths without them) or, a sequence a call, from K and V themselves without norm and rotation.
  */
 int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t *k, const gfwa_heads_t *v, const float *wq,
                       const float *wk, float eps, const double *freq, int rot, int flags, const float *alpha, long long alpha_token,

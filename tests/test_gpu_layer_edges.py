@@ -147,3 +147,65 @@ def test_bench_of_the_paged_step_reads_what_no_cache_holds(g, shape, bound, caps
     between = line["detail"]["caches_in_turn"] * line["detail"]["algorithmic_bytes"]
     assert line["detail"]["caches_in_turn"] >= 2 and line["roofline"]["bound"] == bound and (between >= 512 << 20) == (bound == "hbm")
     assert line["value"] < line["roofline"]["peak"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompts_go_through_the_attention_and_into_the_cache(g, dtype):
+    """A padded batch of prompts: norm and rotation, attention, append without queries; a second chunk of one sequence with a row of the decoding step for
+    each of its tokens; then a token for each sequence.  Outputs against the attention over the whole sequences, the cache against K and V bit for bit."""
+    B, N, H, Hkv, d, page, w, more = 2, 133, 8, 2, 64, 16, 60, 9
+    lens = [133, 70]
+    rng = np.random.default_rng(71)
+    total = N + more + 1
+    x, tx = store(rng.standard_normal((B, total, H + 2 * Hkv, d)), dtype)
+    alpha = gpu((rng.random((B, total, H)) * 0.3).astype(np.float32))
+    wt = gpu((1 + 0.2 * rng.standard_normal((2, d))).astype(np.float32))
+    how, scale = dict(wq=wt[0], wk=wt[1], eps=EPS, freq=dev64(freq_of(d))), d ** -0.5
+    split = lambda t: (t[..., :H, :], t[..., H:H + Hkv, :], t[..., H + Hkv:, :])
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    M = -(-total // page)
+    table = gpu(rng.permutation(B * M).reshape(B, M).astype(np.int32))
+    Kp, Vp = (torch.full((B * M, Hkv, page, d), float("nan"), dtype=TORCH[dtype], device=DEV) for _ in range(2))
+    cp = torch.full((B * M, H, page), float("nan"), device=DEV)
+    # the whole sequences at once; sequence 1 goes on from 70, so its rows there are the later tokens
+    order = [list(range(total)), list(range(lens[1])) + list(range(N, total)) + list(range(lens[1], N))]
+    whole = torch.stack([tx[b, order[b]] for b in range(B)])
+    gates = torch.stack([alpha[b, order[b]] for b in range(B)])
+    Q, K, V = g.gfwa_qk_norm_rope(*split(whole), **how)
+    O, _ = g.gfwa_forward_gqa(Q, K, V, g.gfwa_gate_prefix(gates.transpose(1, 2).contiguous()), w, scale)
+    # two roundings of one formula: scores and weights as in the tests of each
+    bar = 2.0 ** -5 if dtype == "bf16" else 1e-4
+
+    def check(b, p, o):
+        assert (o.float() - O[b, :, p].float()).abs().max() <= bar, (b, p)
+
+    prompt = tx[:, :N].contiguous()
+    q, k, v = split(prompt)
+    Q1, K1, V1 = g.gfwa_qk_norm_rope(q, k, v, **how)
+    O1, _ = g.gfwa_forward_gqa(Q1, K1, V1, g.gfwa_gate_prefix(alpha[:, :N].transpose(1, 2).contiguous()), w, scale)
+    for b in range(B):
+        check(b, lens[b] - 1, O1[b, :, lens[b] - 1])
+    append = lambda x, al, start, cached, tab, **kw: g.gfwa_append_paged(x[1], x[2], Kp, Vp, i32(start), i32(cached), tab, alpha=al, cp=cp, **kw)
+    append(split(prompt.flatten(0, 1)), alpha[:, :N].reshape(B * N, H), [0, N, 2 * N], [0, 0], table, **how)
+    slots = lambda b, n: (table[b].long()[torch.arange(n, device=DEV) // page], slice(None), torch.arange(n, device=DEV) % page)
+    for b in range(B):
+        assert torch.equal(Kp[slots(b, N)], K1[b].transpose(0, 1)) and torch.equal(Vp[slots(b, N)], V1[b].transpose(0, 1))
+    # the same rows already normed and rotated, a sequence a call
+    K2, V2, c2 = torch.zeros_like(Kp), torch.zeros_like(Vp), torch.zeros_like(cp)
+    for b in range(B):
+        g.gfwa_append_paged(K1[b].transpose(0, 1), V1[b].transpose(0, 1), K2, V2, i32([0, N]), i32([0]), table[b:b + 1].contiguous(), norm=False,
+                            alpha=alpha[b, :N], cp=c2)
+        assert all(torch.equal(y[slots(b, N)], z[slots(b, N)]) for y, z in ((Kp, K2), (Vp, V2), (cp, c2)))
+    # nine more tokens of sequence 1, a row of the step for each
+    rows = split(tx[1, N:N + more])
+    Qc = append(rows, alpha[1, N:N + more], [0, more], [lens[1]], table[1:].contiguous(), q=rows[0], **how)
+    o, _ = g.gfwa_decode_paged(Qc, Kp, Vp, cp, table[1:].expand(more, M).contiguous(), i32([lens[1] + i for i in range(more)]), w, scale)
+    for i in range(more):
+        check(1, lens[1] + i, o[i])
+    lens = [N, lens[1] + more]
+    # a token for each
+    rows = split(torch.stack([tx[0, N], tx[1, N + more]]))
+    Qt = append(rows, torch.stack([alpha[0, N], alpha[1, N + more]]), [0, 1, 2], lens, table, q=rows[0], **how)
+    o, _ = g.gfwa_decode_paged(Qt, Kp, Vp, cp, table, i32(lens), w, scale)
+    for b in range(B):
+        check(b, lens[b], o[b])
