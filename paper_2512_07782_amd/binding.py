@@ -297,14 +297,14 @@ def gfwa_append_paged(k: torch.Tensor, v: torch.Tensor, Kp: torch.Tensor, Vp: to
 
 
 def gfwa_decode_paged_workspace_bytes(B: int, H: int, Hkv: int, d: int, page: int, max_pages: int, w: int) -> int:
-    return int(load_library().gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, int(w)))
+    return int(load_library().gfwa_decode_paged_workspace_bytes(B, H, Hkv, d, page, max_pages, max(0, min(int(w), 2 ** 31 - 1))))
 
 
 def gfwa_decode_paged(q: torch.Tensor, Kp: torch.Tensor, Vp: torch.Tensor, cp: torch.Tensor, table: torch.Tensor, pos: torch.Tensor,
                       w: int, scale: float, o: Optional[torch.Tensor] = None, L: Optional[torch.Tensor] = None,
                       workspace: Optional[torch.Tensor] = None):
     """One decoding step against a paged cache (gfwa_append_paged's): q [B,H,d] at positions pos [B] int32, whose keys are appended
-    already; -1: a slot without a sequence (o = 0, L = -inf).  Returns o [B,H,d], L [B,H]."""
+    already; -1: a slot without a sequence (o = 0, L = -inf).  w: any whole number from 1 on.  Returns o [B,H,d], L [B,H]."""
     return (_call or _native()).decode_paged(q, Kp, Vp, cp, table, pos, w, scale, o, L, workspace)
 
 

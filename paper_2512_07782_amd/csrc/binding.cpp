@@ -161,6 +161,16 @@ int as_int(PyObject* o) {
     if (PyErr_Occurred()) throw PyError{};
     return (int)(unsigned)v;
 }
+// A window of a cache whose positions are C ints: longer ones hold every sequence, as the longest int does.
+int as_window(PyObject* o) {
+    PyObject* n = PyNumber_Long(o);
+    if (n == nullptr) throw PyError{};
+    int past = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(n, &past);
+    Py_DECREF(n);
+    if (v == -1 && !past && PyErr_Occurred()) throw PyError{};
+    return past > 0 || v > 0x7fffffffLL ? 0x7fffffff : past < 0 || v < 1 ? 0 : (int)v;  // 0: refused
+}
 float as_float(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw PyError{};
@@ -708,7 +718,7 @@ PyObject* decode_paged(PyObject* const* a) {  // q, Kp, Vp, cp, table, pos, w, s
     if (a[3] == Py_None) fail(PyExc_TypeError, "cp must be a tensor");
     const Pages cache(a[1], a[2], a[3], a[4], B, H, Hkv, d, q.scalar_type(), dev, false);
     const void* pos = dense(a[5], bs, at::kInt, dev, "pos").const_data_ptr();
-    const int w = as_int(a[6]);
+    const int w = as_window(a[6]);
     const float scale = as_float(a[7]);
     for (int i = 8; i < 11; ++i)
         if (a[i] != Py_None) dev.also(tensor_of(a[i], "an output"), "an output");

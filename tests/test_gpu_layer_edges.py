@@ -209,3 +209,17 @@ def test_prompts_go_through_the_attention_and_into_the_cache(g, dtype):
     o, _ = g.gfwa_decode_paged(Qt, Kp, Vp, cp, table, i32(lens), w, scale)
     for b in range(B):
         check(b, lens[b], o[b])
+
+
+def test_decode_windows_past_32_bits(g):
+    """A window longer than any position holds every sequence, however long it is; none below one is taken."""
+    rng, table, Kp, Vp, cp = paged_case(3, [(64, 0)], 4, 2, 64, 16, "bf16", M=4)
+    args = store(rng.standard_normal((1, 4, 64)), "bf16")[1], store(Kp, "bf16")[1], store(Vp, "bf16")[1], gpu(cp), gpu(table), gpu(np.array([60], dtype=np.int32))
+    want = g.gfwa_decode_paged(*args, 64, 0.125)
+    for w in (2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, 2 ** 63, 2 ** 70 + 1):
+        assert g.gfwa_decode_paged_workspace_bytes(1, 4, 2, 64, 16, 4, w) == g.gfwa_decode_paged_workspace_bytes(1, 4, 2, 64, 16, 4, 64) > 0
+        assert all(torch.equal(a, b) for a, b in zip(g.gfwa_decode_paged(*args, w, 0.125), want)), w
+    for w in (0, -1, -2 ** 32 + 7, -2 ** 70):
+        assert g.gfwa_decode_paged_workspace_bytes(1, 4, 2, 64, 16, 4, w) == 0
+        with pytest.raises(g.GfwaError):
+            g.gfwa_decode_paged(*args, w, 0.125)
