@@ -3,7 +3,7 @@
 //   * rows of queries, keys and values are held and worked on as in qk_norm_rope.hip; a row's sequence is looked up from the batch's
 //     offsets and its page from the table, once for all its heads;
 //   * the prefix is a scan along each sequence and goes to workgroups of its own, which the launch begins with (us, H 32, Hkv 8, d 128, one prompt of
-//     8192 tokens: a wave for each head 83, in segments 50, without gates 43; 16 prompts of up to 2048 tokens 101 either way).
+//     8192 tokens: without gates 40.9, with the prefix in segments 48.4, by a wave for eight heads 190; 16 prompts of up to 2048 tokens 95.7 and 98.4).
 #include "gfwa_internal.h"
 #include "head_rows.h"
 
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const A
         Angles angles;
         auto look_up = [&]() __attribute__((always_inline)) {
             if (b != -2) return;
-            Frequencies freq;  // here, not in front of the loop: that takes three waves a SIMD where four have room (7168 tokens 48 us, 39)
+            Frequencies freq;  // here, not in front of the loop: that takes three waves a SIMD where four have room (7168 tokens 47.3 us, 41.8)
             const bool turned = range.x0 < values && a.rot > 0;
             if (turned) freq.load(l, a.freq);
             int first, before;
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_paged_kernel(const A
                     r.arrive();
                     r.norm_and_turn(l, a.norm, a.eps, w, a.rot > 0, a.paired, angles);
                 }
-                const int h = h0 + i * HG + side;  // (with h0 + i * HG + x in its place: 16 prompts 98.8 us, 97.4)
+                const int h = h0 + i * HG + side;  // (with h0 + i * HG + x in its place: 16 prompts 97.2 us, 95.7)
                 r.template store<ONCE>([&](int x) __attribute__((always_inline)) { return to + (h + (x - side)) * step; },
                                        [&](int x) __attribute__((always_inline)) { return there && h + (x - side) < h1; }, side, l, K != kValues);
             });
@@ -315,8 +315,9 @@ hipError_t append_paged(bool bf16, const HeadsView& q, const HeadsView& k, const
     constexpr int kThreads = 64 * kAppendWaves;
     // The prefix.  Where sequences bring two tokens or fewer on average a wave takes eight heads of a sequence, however many tokens that has; otherwise a
     // workgroup does, for a segment of it: of 512 tokens, or as many as keep the segments to 64 and all sequences' to about 1024 workgroups.  (us, H 32,
-    // Hkv 8, d 128, waves / workgroups: 512 sequences of two tokens 10.5 / 13.4, 256 of four 10.0 / 11.1, 299 of one and one of 512 17.4 / 9.9; 16 prompts in
-    // up to 4096 workgroups 100.6, in up to 1024 98.3.)
+    // Hkv 8, d 128, waves / workgroups: 512 sequences of two tokens 10.2 / 13.3, 256 of four 9.9 / 11.5, 299 of one and one of 512 18.0 / 11.3; 16 prompts in
+    // up to 4096 workgroups 97.4, in up to 1024 95.7.)  Among many sequences a long one then is a single workgroup's for eight heads: one of 8192 tokens beside 31
+    // of one 55.8, beside 255 80.0 (without gates 49.4 and 52.3; the 256 in up to 4096 workgroups 59.0).
     const int units = (H + kScanHeads - 1) / kScanHeads, sequences = B * units;
     if (alpha != nullptr && rows > 2LL * B) {
         const int most = sequences < 1024 ? 1024 / sequences : 1, want = (rows + kScanTokens - 1) / kScanTokens;

@@ -36,8 +36,8 @@ struct PagedArgs {
 
 // Tiles of a chunk of a window of `tiles`: what the longest window is cut into; but a sequence of less than an eighth of that (a table has columns
 // for the longest one there may be) is cut into all the chunks there are, none smaller than the least.  (Eight sequences of 1000 tokens, H 32, Hkv 8,
-// d 128, without a window in a table for 131072: 21.8 us in one chunk each, 11.7 in five.  Every sequence like that: 16 of up to 8192 in fp32 126 us
-// against 123.)
+// d 128, without a window in a table for 131072: 24.4 us in one chunk each, 13.5 in five.  Every sequence like that: 16 of up to 8192 in fp32 127 us
+// against 125.)
 __device__ __forceinline__ int chunk_of(const PagedArgs& a, int tiles) {
     if (tiles >= a.chunk * (long long)a.splits / 8) return a.chunk;
     const int c = ((tiles + a.splits - 1) / a.splits + a.waves - 1) / a.waves * a.waves;
@@ -77,7 +77,7 @@ struct Tile;
 // bf16 (16x16x32): two units make the 32 keys of the second product.  V^T goes through LDS, which hands out transposed pieces in P's order, 16-byte chunks
 // permuted so that neither the row-wise writes nor the transposed reads meet in a bank.  A weight enters the product as two bf16 numbers, cut off and the
 // rest, off by 2^-16 of it at most: one alone would be off by 2^-8, as much as the output's own rounding (against fp64, norm of the difference 1.9e-3 to
-// 2.6e-3 instead of 1.7e-3; 64 sequences, w 1024, 46.6 us either way, one 7.9 and 7.8).  Neither part is negative, and the rest of a weight that is not zero is not
+// 2.6e-3 instead of 1.7e-3; 64 sequences, w 1024, 45.2 us with one, 45.4 with two, one 7.6 and 7.75).  Neither part is negative, and the rest of a weight that is not zero is not
 // zero either (2^-133 at least): an infinity among the values stays one, where the rest of a rounded weight would make 0 inf or inf - inf of it.  The matrix cores
 // take 384 of the about 1700 cycles that a compute unit's share of the memory's rate gives the tile's 16 KiB (D = 128).
 template <int D>
@@ -246,12 +246,12 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // the next tile are on their way while a tile is worked on.  A head's weights are taken against a reference that is raised, and sums rescaled,
 // only when a score exceeds it by 2^16.
 // (The page numbers of the tile after that could be asked for ahead too: eight more registers, which bf16 at d = 128 does not have beside three waves a
-// SIMD; whole sequences, H 32, Hkv 8, 4 of up to 8192 22.3 us with and 19.5 without, 16 of them 68.3 and 65.4, 128 windows of 512 keys 49.3 and 51.7.
-// Two tiles ahead: 22.1, 68.1 and 47.6, in fp32 past the registers.)
-// ONCE: V is loaded past the caches.  No other workgroup reads it, and a window that the L2s do not hold is read faster (us, bf16, H 32, Hkv 8, d 128,
-// w 1024: 64 sequences 48.7 -> 46.3, 32 26.4 -> 22.5, 12 that no cache holds 16.9 -> 16.2; fp32, 64 sequences 91 -> 85; H 32, Hkv 4, d 64, whole
-// sequences of up to 16384 40.6 -> 35), one that they do hold more slowly (2 sequences of H 16, d 64, w 512, 4 MB, 6.7 -> 7.2).  K's lines are asked for
-// by two loads each: past the caches the 64 sequences take 47.6.
+// SIMD; when it was tried, whole sequences, H 32, Hkv 8, 4 of up to 8192 took 22.3 us with and 19.5 without, 16 of them 68.3 and 65.4, 128 windows of 512 keys
+// 49.3 and 51.7.  Two tiles ahead: 22.1, 68.1 and 47.6, in fp32 past the registers.)
+// ONCE: V is loaded past the caches.  No other workgroup reads it, and windows that no cache holds are read faster (us, bf16, H 32, Hkv 8, d 128,
+// w 1024: 64 sequences 48.3 -> 45.4, 32 26.1 -> 22.4; fp32, 64 sequences 90 -> 83; H 32, Hkv 4, d 64, whole sequences of up to 16384 40.6 -> 34.3), those that
+// the memory-side cache holds from call to call more slowly (12 sequences in three sets, 143 MB, 14.5 -> 15.0).  K's lines are asked for by two loads each:
+// past the caches the 64 sequences take 48.3.
 template <typename T, int D, int NW, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArgs a) {
     typedef Tile<T, D> Tl;
@@ -424,8 +424,8 @@ __global__ __launch_bounds__(64 * NW, 2) void decode_paged_kernel(const PagedArg
 
 // o = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),  L = (M + log2 of that sum) ln 2
 // over the chunks.  NG groups of D threads take every NG-th record each.  Up to kFewChunks every chunk leaves a record, without sums where it holds
-// nothing of the window; of more than that only those that do, and the merge asks for the position (one conversation, w 1024, nine chunks: 0.3 us
-// less without the look; whole sequences, 65 chunks: 3 us more).
+// nothing of the window; of more than that only those that do, and the merge asks for the position (H 32, Hkv 8, w 1024: without the look one
+// conversation, nine chunks, 7.75 us instead of 7.84, eight 12.0 instead of 12.6; 16 whole sequences of H 32, Hkv 4, d 64 35.6 instead of 34.3).
 template <typename T, int D, int NG>
 __global__ __launch_bounds__(D * NG) void decode_paged_combine_kernel(const PagedArgs a) {
     __shared__ float sm_o[NG][D], sm_m[NG], sm_l[NG];
@@ -507,11 +507,13 @@ struct Plan {
         waves = 4;
         // Measured (us, four and eight waves, graphs of 21 steps; H 32, Hkv 8, d 128 unless named):
         //   * a window shorter than the table is about as long for every sequence.  Where one chunk each gives every compute unit two
-        //     workgroups of four waves that is best (64 sequences, w 1024: one chunk 46, two 53); with half of that, one of eight
-        //     waves (32 sequences: 22.5; two chunks of four waves 25.4); with fewer, chunks for two workgroups (8: 12.1, for one 13.4).
+        //     workgroups of four waves that is best (64 sequences, w 1024: one chunk 45, two 53); with half of that, one of eight
+        //     waves (32 sequences: 22.4; two chunks of four waves 25.2); with fewer, chunks for two workgroups (8: 12.0, for one 13.2).
         //   * whole sequences are of any length: chunks of two tiles a wave, or as many as make 4096 workgroups, level that (16 of up
-        //     to 8192: 66; 512 workgroups 81; H 32, Hkv 4, d 64, up to 16384: 35 and 47).
-        //   * a window of three tiles a wave is not worth the merge (300 keys of one sequence: 4.6, in three chunks 6.1).
+        //     to 8192: 64; 512 workgroups 80; H 32, Hkv 4, d 64, up to 16384: 34 and 47).
+        //   * a window of up to three tiles a wave goes in one chunk, without a merge: w 200, 300, 700 (one chunk / chunks of four waves) of 31 sequences
+        //     8.4 / 11.3, 10.4 / 13.2, 17.2 / 20.0, of 16 7.3 / 9.2, 8.6 / 10.3, 14.7 either way, of 8 6.2 / 7.8, 8.5 either way, 13.3 / 10.6, of one 6.1 / 7.1,
+        //     7.7 / 7.1, 11.9 / 7.3: up to about eight sequences windows of two and three tiles a wave would be better off in chunks.
         const bool even = w < (long long)max_pages * page;
         long long S = 1;
         least = waves;

@@ -196,9 +196,10 @@ struct LaneVector {
 };
 
 // The two units of a lane's row.
-// ONCE: loaded past the caches (bf16, where a load takes whole lines).  Large inputs are read faster (us, H 32, Hkv 8, d 128, N 16384: forward 84 -> 81,
-// backward 122 -> 120; append of 16 prompts 107 -> 103; forward of N 4096, 50 MB, 23.3 -> 21.8; B 4, H 16, N 4096, d 64 43.2 -> 40.6), those that are small
-// enough to be held from their making more slowly (N 2600, 32 MB, 13.7 -> 16.6; H 16, Hkv 4, N 4100, 25 MB, backward 19.4 -> 22.3).
+// ONCE: loaded past the caches (bf16, where a load takes whole lines).  Large inputs are read faster (us, through / past the caches: forward of H 32, Hkv 8,
+// d 128, N 4096, 50 MB, 21.2 / 20.4, of B 4, H 16, Hkv 4, N 4096, d 64 22.5 / 21.8, append of 16 prompts 103.6 / 96.4, backward of H 32, Hkv 8, N 16384
+// 120.5 / 118.0), those that are small enough to be held from their making more slowly (forward of N 2600, 32 MB, 13.1 / 14.9; backward of H 16, Hkv 4,
+// N 4100, 25 MB, 18.8 / 21.5).
 // Forward and append count what they read (through / past the caches: append without queries, H 32, Hkv 8, d 128, 8100 tokens, 33 MB, 15.1 / 19.0,
 // forward without values, H 16, Hkv 16, N 4100, 34 MB, 14.7 / 16.7).
 constexpr long long kOnceBytes = 40 << 20;  // inputs of more than this are loaded past the caches: the L2s hold 32 MiB
@@ -209,8 +210,8 @@ struct LaneRow {
     // row(s): the row of the lanes with the same place in their rows and side s.
     // kPair: rows of 128 bytes, of which a load of one unit by a row's four lanes takes half a line.  So the rows of sides 2 i and 2 i + 1 are loaded and stored
     // one after the other, each by the lanes of both, unit a by the even side's and b by the odd one's, and arrive() gives every lane its own row's (us, halves /
-    // whole lines: forward of B 4, H 16, Hkv 4, d 64, N 4200 29.6 / 24.3, of H 32, Hkv 4, N 16384 40.6 / 32.4, gradients of N 4200 43.9 / 37.3, append of 40000
-    // tokens 69.5 / 60.3; N 2048, 25 MB, forward 11.9 / 12.3).  PAIR false: not worth it, for the derivative's inputs through the caches.
+    // whole lines: forward of B 4, H 16, Hkv 4, d 64, N 4200 30.9 / 23.8, of H 32, Hkv 4, N 16384 37.8 / 31.2, gradients of N 4200 42.2 / 37.3, append of 40000
+    // tokens 65.8 / 58.8; N 2048, 25 MB, forward 11.5 / 12.0).  PAIR false: not worth it, for the derivative's inputs through the caches.
     template <typename Row>
     __device__ __forceinline__ void load(Row&& row, int side, const LaneOfRow<D>& l) {
         if constexpr (kPair) {
@@ -226,9 +227,10 @@ struct LaneRow {
     __device__ __forceinline__ void arrive() {
         if constexpr (kPair) exchange();
     }
-    // PAST: stored past the caches, for what nothing reads soon.  (The cache's new rows: 16 prompts 109 -> 103 us.  The results of norm and rotation would
-    // cost less themselves, us, H 32, Hkv 8, N 16384: forward 85 -> 83, backward 120 -> 117, and the kernel that reads them right after more: rope
-    // and attention in a row 226 -> 233, at B 4, H 16, Hkv 4, N 4096, d 64 73 -> 78, the backward and a matrix product with its result 407 -> 412.)
+    // PAST: stored past the caches, for what nothing reads soon.  (The cache's new rows: 16 prompts 105.7 -> 95.9 us.  The results of norm and rotation would
+    // cost less themselves, us, H 32, Hkv 8, N 16384: forward 77.9 -> 74.0, backward 119 -> 116, and the kernel that reads them right after more: rope
+    // and attention in a row (w 1024) 217 -> 225, at B 4, H 16, Hkv 4, N 4096, d 64 (w 512) 75.6 -> 76.4, the backward and a matrix product with its result
+    // 419 -> 423.)
     // there(s): whether side s's row is to be written.  Called once a row; arrived: after arrive()
     template <bool PAST, typename Row, typename There>
     __device__ __forceinline__ void store(Row&& row, There&& there, int side, const LaneOfRow<D>& l, bool arrived = true) {
@@ -277,9 +279,10 @@ struct LaneRow {
 };
 
 // Heads of a token that a wave takes side by side: what it reads of a token-major tensor comes in runs of kSide rows, what it writes of a head-major one in
-// runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16640, d 128 96 / 97 / 90 / 84, backward 151 / 142 / 125 /
-// 119, of N 16384 133 / 125 / 120 / 123, of H 16, Hkv 4, N 4100 21 / 21 / 22 / 30, append of 16 prompts 114 / 108 / 101 / 105; rows of 4 lanes, two / four heads,
-// B 4, H 16, Hkv 4, d 64: forward of N 4096 22.4 / 20.4, of N 4200 24.3 / 26.2, of N 2048 12.3 / 13.2, backward of N 4096 33.6 / 35.9, of N 4200 37.6 / 41.3.)
+// runs of its tokens.  (us, rows of 8 lanes, one / two / four / eight heads: forward of H 32, Hkv 8, N 16640, d 128 100 / 97 / 89 / 83, backward 152 / 140 / 126 /
+// 119, of N 16384 131 / 124 / 118 / 118, of H 16, Hkv 4, N 4100 19.6 / 18.7 / 18.9 / 25.4, append of 16 prompts 123 / 113 / 96 / 98; rows of 4 lanes, two / four
+// heads, B 4, H 16, Hkv 4, d 64: forward of N 4096 22.2 / 20.3, of N 4200 23.6 / 25.7, of N 2048 11.8 / 12.5, backward of N 4096 32.3 / 34.8, of N 4200
+// 37.2 / 40.8.)
 template <int D>
 constexpr int kSide = D == 128 ? 4 : 2;
 

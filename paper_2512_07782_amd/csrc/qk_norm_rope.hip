@@ -16,9 +16,11 @@ namespace {
 
 constexpr int kRopeWaves = 4;  // waves of a workgroup, each on its own
 
-// Forward: eight heads side by side where the queries and the keys have a multiple of eight and more than 128 MiB are read; what a wave reads is then one
-// token's (us, kSide / eight: H 32, Hkv 8, d 128, N 32768 174 / 155, 16384 88 / 81, 12000 65 / 62, 8192 41.5 / 42.2, 4096 22.8 / 22.7, 1024 10.2 / 10.9;
-// B 8, H 16, N 8192, d 64 164 / 157; fp32, B 2, H 16, N 4400 100 / 93).
+// Forward: eight heads side by side where the queries and the keys have a multiple of eight and the projection has more than 128 MiB; what a wave reads is then
+// one token's (us, kSide / eight: H 32, Hkv 8, d 128, N 32768 175 / 148, 16384 84.0 / 78.0, 12000 63.3 / 60.8, 8192 37.1 / 38.9, 4096 20.3 / 21.4; B 8, H 16,
+// Hkv 16, N 8192, d 64 150 / 151; fp32, B 2, H 16, Hkv 16, N 4400 97 / 90).  Without a multiple of eight, H 32, Hkv 4, d 128: N 13500 59.1 / 60.5, 16384
+// 72.8 / 69.7, 32768 140 / 132; H 12, Hkv 4, N 27000 56.8 / 66.4; H 14, Hkv 2, N 30000 59.7 / 71.6.  Without values the projection counts all the same (H 16,
+// Hkv 16, d 128, N 12000, 98 MB read, 39.0 / 37.9; d 64, B 4, N 5700 34.6 / 35.7).
 constexpr int kManySide = 8;
 constexpr long long kManyBytes = 128 << 20;
 
@@ -104,11 +106,14 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_norm_rope_kernel(const Rop
     }
 }
 
-// By the size of the inputs (bf16): of more than kOnceBytes gradients are read past the caches; between kInputsBytes and kManyBytes the inputs too (three
+// By the size of the projection (bf16): of more than kOnceBytes gradients are read past the caches; between kInputsBytes and kManyBytes the inputs too (three
 // tensors of that size pass the memory-side cache); of more than kManyBytes rows of four lanes are taken four side by side.  (us, inputs through / past the
-// caches: H 32, Hkv 8, d 128, N 6000, 74 MB, 42.7 / 44.9, 8192 63.3 / 56.4, 12000, that no cache holds, 88.7 / 89.4, 16384 119 / 123; d 64, H 32, Hkv 4,
-// N 16384, 84 MB, 58.4 / 49.6, B 4, H 16, Hkv 4, N 4096 33.0 / 34.0; four side by side instead of two: B 8, H 16, N 8192 216 -> 207, B 4, H 16, Hkv 4,
-// N 4096 33.6 -> 35.9.)
+// caches, calls on three sets of tensors in turn: H 32, Hkv 8, d 128, N 4096 31.4 / 31.1, 6000, 74 MB, 50.7 / 43.5, 6500 55.5 / 50.8, 8192 62.9 / 61.6, 12000, that
+// no cache holds, 89.2 / 89.3, 16384 118 / 123; d 64, H 32, Hkv 4, N 16384, 84 MB, 55.9 / 48.2, B 4, H 16, Hkv 4, N 4096 31.7 / 33.1, 5500, 68 MB, 47.3 / 41.1;
+// results in the same memory each time: N 6000 42.3 / 44.0, 6500 49.4 / 50.6, 8192 55.0 / 55.2, d 64, N 5500 40.1 / 40.8.  Four side by side instead of two:
+// B 8, H 16, Hkv 16, N 8192 216 -> 208, B 4, H 16, Hkv 4, N 4096 31.7 -> 35.1.)
+// The values' heads count, given or not: by what is read alone, H 16, Hkv 16, d 128, N 8192 without dV would take 48.0 instead of 42.6, H 32, Hkv 8, N 12000 84.5
+// instead of 82.2.
 enum BwdSize { kSmall = 0, kMiddle = 1, kSpread = 2, kLarge = 3 };
 constexpr long long kInputsBytes = 72 << 20;
 template <int D, int SIZE>
@@ -248,8 +253,8 @@ __global__ __launch_bounds__(1024) void weight_grad_sum_kernel(const float* __re
 }
 
 // Workgroups that leave sums of the weights' gradients.  In bf16 three waves a SIMD are there at a time, and what fits in them goes at once; more goes through
-// two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 120 / 122 / 124, B 4, H 16, N 8192 207 /
-// 212 / 218; 513 workgroups' worth, H 16, Hkv 4, N 4100, 19.4 with up to 768, 23.6 with 512).  In fp32 two waves a SIMD are all there are (512 / 768 workgroups,
+// two waves a SIMD, which meet memory in longer runs (us, 512 / 768 / 2048 workgroups: H 32, Hkv 8, N 16384, d 128 118 / 119 / 122, B 4, H 16, Hkv 16, N 8192
+// 207 / 211 / 219; 513 workgroups' worth, H 16, Hkv 4, N 4100, 22.7 / 18.7 / 18.7).  In fp32 two waves a SIMD are all there are (512 / 768 workgroups,
 // d 128: H 8, Hkv 2, N 5000 25.7 / 28.3, H 16, Hkv 4, N 6100 51.5 / 57.2, N 4200 44.5 / 44.6, H 32, Hkv 8, N 5000 83.0 / 82.2).
 constexpr int kMostSums = 768, kManySums = 512;
 
