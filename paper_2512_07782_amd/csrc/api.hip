@@ -120,19 +120,29 @@ struct HeadsSpan {
         bool holds(long long at, int d) const {
             if (at < 0) return false;
             for (int i = 2; i >= 0; --i)
-                if (dims[i][1] > 1) at -= dims[i][0] * std::min(at / dims[i][0], dims[i][1] - 1);
+                if (dims[i][1] > 1 && at >= dims[i][0]) at -= dims[i][0] * std::min(at / dims[i][0], dims[i][1] - 1);
             return at < d;
         }
     };
-    bool rows_disjoint(int B, int N, int d) const { return !t || Nest(*t, B, N, heads).disjoint(d); }
+    Nest nest(int B, int N) const { return Nest(*t, B, N, heads); }
     // whether its first or last row meets a row of o, a tensor of disjoint rows
-    bool ends_meet(const HeadsSpan& o, int B, int N, int d, size_t size) const {
-        if (!t || !o.t) return false;
+    bool ends_meet(const HeadsSpan& o, const Nest& rows, int B, int N, int d, size_t size) const {
         const long long first = ((intptr_t)t->data - (intptr_t)o.t->data) / (long long)size, last = first + last_row(B, N);
-        const Nest rows(*o.t, B, N, o.heads);
         return rows.holds(first, d) || rows.holds(first + d - 1, d) || rows.holds(last, d) || rows.holds(last + d - 1, d);
     }
 };
+
+// whether outputs of one call are strided so that none of their rows meet
+static bool rows_apart(const HeadsSpan* outs, int count, int B, int N, int d, size_t size) {
+    for (int i = 0; i < count; ++i) {
+        if (!outs[i].t) continue;
+        const HeadsSpan::Nest rows = outs[i].nest(B, N);
+        if (!rows.disjoint(d)) return false;
+        for (int j = 0; j < count; ++j)
+            if (j != i && outs[j].t && outs[j].ends_meet(outs[i], rows, B, N, d, size)) return false;
+    }
+    return true;
+}
 
 static HeadsView view(const gfwa_heads_t* t) { return t ? HeadsView{t->data, t->batch, t->token, t->head} : HeadsView{nullptr, 0, 0, 0}; }
 
@@ -391,13 +401,9 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t* q, const gfw
     const HeadsSpan ins[] = {{q, H}, {k, Hkv}}, outs[] = {{dq, H}, {dk, Hkv}, {dv, Hkv}};
     for (const HeadsSpan& x : ins)
         if (int r = x.check(B, N, d, size)) return r;
-    for (const HeadsSpan& x : outs) {
-        if (int r = x.check(B, N, d, size)) return r;
-        if (!x.rows_disjoint(B, N, d)) return GFWA_ERR_OVERLAP;
-    }
     for (const HeadsSpan& x : outs)
-        for (const HeadsSpan& o : outs)
-            if (&x != &o && x.ends_meet(o, B, N, d, size)) return GFWA_ERR_OVERLAP;
+        if (int r = x.check(B, N, d, size)) return r;
+    if (!rows_apart(outs, 3, B, N, d, size)) return GFWA_ERR_OVERLAP;
     const Bytes grads[] = {{dQ, bytes * H}, {dK, bytes * Hkv}, {dV, bytes * Hkv}};
     for (const Bytes& g : grads)
         if (!aligned(g.at, 16)) return GFWA_ERR_ALIGN;
