@@ -6,6 +6,7 @@
  * (outputs, cache, workspace) may not overlap what it reads, nor each other, judged by the ranges of bytes that the tensors span:
  * GFWA_ERR_OVERLAP (dq, dk and dv among each other are the one exception: there the first and last rows of each are looked for among the others' rows).
  * A workspace belongs to its call until that is done on the stream: calls that may run at the same time (two streams, two captured graphs) need one each.
+ * Sizes: N (new tokens of a call) up to 2^24, B * H up to 2^24 (2^22 with a paged cache), B * H * ceil(N / 32) and B * N below 2^31: GFWA_ERR_DIM.
  */
 #ifndef GFWA_LAYER_H
 #define GFWA_LAYER_H
@@ -41,7 +42,8 @@ enum {
  *
  * where p is the token's position and (i, j) is (m, m + rot/2), or (2m, 2m + 1) with GFWA_ROPE_PAIRED; dimensions from rot
  * on are not rotated.  Rows of v change their place alone.  fp32 arithmetic, rounded once; the angle is formed and
- * reduced in fp64.
+ * reduced in fp64.  Squares are fp32 numbers too: a row whose squares add up to more than 3.4e38 comes out as zeros, and with eps = 0 one
+ * whose squares are all below 2^-149 as infinities or NaN.
  *
  * q: [B,N,H,d], k, v: [B,N,Hkv,d] of dtype `dt`, strided;  v may be NULL (V is then ignored).
  * wq, wk: [d] fp32 or NULL.  freq: [rot/2] fp64 in device memory, 8-byte aligned, in radians for each position; rot: a multiple of
@@ -99,7 +101,8 @@ int gfwa_qk_norm_rope_backward(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfw
  * Rows 0 .. rows-1 alone are there: where start begins in front of row 0 or ends behind the last row, the others' tokens are passed over.
  * Rows that belong to no sequence (in front of start[0], from start[B] on) are left out: their rows of Q stay as they were.  Of rows whose
  * position lies outside the table, or in a page that is not there, the query alone is written.
- * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page.
+ * Q: [rows,H,d] of dtype `dt`, dense, out.  Two sequences must not append to one page, and what cached counts is in the cache before the call: none
+ * of it may be a new token of another sequence of the same call (a prompt in two pieces takes two calls).
  *
  * What reads Q: gfwa_decode_paged, a query for each of its rows.  In a decoding step these are the batch's; of several new tokens every one
  * can be a row there, with its sequence's row of the table and its own position, which reads each one's window.  gfwa_forward_gqa reads no
@@ -127,6 +130,7 @@ int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t
  * gfwa_decode_paged_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after.
  * Only the window is read: 2 * min(w, p+1) * d cache elements per key/value head, once for up to 16 query heads.
  */
+/* (the query: 0 on invalid sizes) */
 size_t gfwa_decode_paged_workspace_bytes(int B, int H, int Hkv, int d, int page, int max_pages, int w);
 int gfwa_decode_paged(gfwa_dtype_t dt, const void *q, const void *Kp, const void *Vp, const float *cp, const int *table,
                       const int *pos, void *o, float *L, void *workspace, size_t workspace_bytes, int B, int H, int Hkv, int d,

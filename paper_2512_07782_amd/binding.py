@@ -292,7 +292,8 @@ def gfwa_append_paged(k: torch.Tensor, v: torch.Tensor, Kp: torch.Tensor, Vp: to
     """Append new tokens to a paged cache: rows start[b] .. start[b+1] of k, v [rows,Hkv,d] (and q [rows,H,d], strided as in
     gfwa_qk_norm_rope) go to positions cached[b] on of sequence b, normed and rotated; with alpha [rows,H] (any strides) the gate prefix is
     carried on in cp.  Kp, Vp [pages,Hkv,page,d], cp [pages,H,page] fp32, table [B,max_pages] int32; start [B+1], cached [B] int32.
-    Returns Q [rows,H,d] (None without q); rows of no sequence are left as they are (a fresh Q: undefined)."""
+    Returns Q [rows,H,d] (None without q), queries for gfwa_decode_paged; rows of no sequence are left as they are (a fresh Q: undefined).
+    A prompt goes through gfwa_qk_norm_rope and the attention and is appended without q.  No token that cached counts may be new in the same call."""
     return (_call or _native()).append_paged(k, v, Kp, Vp, start, cached, table, q, wq, wk, eps, freq, norm, paired, alpha, cp, Q)
 
 

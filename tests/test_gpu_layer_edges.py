@@ -223,3 +223,20 @@ def test_decode_windows_past_32_bits(g):
         assert g.gfwa_decode_paged_workspace_bytes(1, 4, 2, 64, 16, 4, w) == 0
         with pytest.raises(g.GfwaError):
             g.gfwa_decode_paged(*args, w, 0.125)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_squares_leave_32_bits(g, dtype):
+    """Squares are taken in 32 bits: rows that overflow them come out as zeros, and so do their gradients; their neighbours do not change."""
+    rng = np.random.default_rng(81)
+    x = rng.standard_normal((1, 5, 2, 64))
+    big = x.copy()
+    big[0, 2, 1] = 1e20 * np.sign(x[0, 2, 1])
+    (x, t), (big, tb) = store(x, dtype), store(big, dtype)
+    f = dev64(freq_of(64))
+    Q, K, _ = g.gfwa_qk_norm_rope(t, t, freq=f)
+    Qb, _, _ = g.gfwa_qk_norm_rope(tb, t, freq=f)
+    grads = g.gfwa_qk_norm_rope_backward(t, t, Q, K, freq=f)[0], g.gfwa_qk_norm_rope_backward(tb, t, Q, K, freq=f)[0]
+    assert (Qb[0, 1, 2] == 0).all() and (grads[1][0, 2, 1] == 0).all()
+    Qb[0, 1, 2], grads[1][0, 2, 1] = Q[0, 1, 2], grads[0][0, 2, 1]
+    assert torch.equal(Q, Qb) and torch.equal(*grads)
