@@ -126,6 +126,8 @@ int gfwa_append_paged(gfwa_dtype_t dt, const gfwa_heads_t *q, const gfwa_heads_t
  * q: [B,H,d] of dtype `dt`, dense.  pos: [B] int32 in device memory; a position past the table is taken as its last one.  pos[b] < 0,
  * or a page of position p that is not there: the sequence has no token, o = 0 and L = -inf; so it is where every score is minus
  * infinity (scores below -2e38 count as that).
+ * An infinite v_i whose weight softmax_i is not below 2^-126 of the largest is the result of its column, as the definition has it; below that its
+ * weight is zero, and the column NaN.  Weights stand up to 2^16 above one on the way: finite values beyond about 2^100 may come out as infinities.
  * o: [B,H,d] of dtype `dt`, out.  L: [B,H] fp32 out, may be NULL.  workspace: device scratch of at least
  * gfwa_decode_paged_workspace_bytes(...) bytes, 16-byte aligned, contents undefined before and after.
  * Only the window is read: 2 * min(w, p+1) * d cache elements per key/value head, once for up to 16 query heads.
